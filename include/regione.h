@@ -241,6 +241,57 @@ int regione_pack_weight_fp8(regione_ctx* ctx, const void* wq /*[n,k] uint8 row-m
 int regione_linear_fp8(regione_ctx* ctx, const void* xq, const float* x_scale, const void* wq_packed, const float* w_scale,
                        const float* b_opt, int32_t m, int32_t n, int32_t k, int32_t act, int32_t out_dtype, void* y);
 
+/* 4-bit variant of the dense projections: MXFP4 of the OCP microscaling specification.  An extension with its own
+ * accuracy like the 8-bit variant, never chosen silently.  32 consecutive values of a row share a power of two:
+ *   amax = max |x|,  e = max(floor(log2 amax) - 2, -127)  (-127 for a block of zeros),  scale byte e + 127,
+ *   code = x / 2^e rounded to the nearest E2M1 value, ties to the even code, magnitudes above 6 to 6,
+ * E2M1: bit 3 the sign, bits 2..0 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Two codes per byte, the lower column in the lower
+ * four bits.  A block that holds a NaN or an infinity gets scale byte 255 (NaN) and zero codes.
+ *
+ * Scales lie in one of two layouts:
+ *   REGIONE_MX_SCALE_ROWS  [rows, cols / 32] bytes, as the specification's tensors are usually kept;
+ *   REGIONE_MX_SCALE_STEPS what the products read: for every step of 256 columns, the rows (rounded up to an even
+ *     number) of eight bytes; block b of a step at byte 2 * (b % 4) + b / 4; blocks past the row's end are zero (the
+ *     quantiser writes them).
+ * regione_mxfp4_scale_bytes gives the size of either.
+ *
+ * regione_quantize_rows_mxfp4: x [rows, cols] (bf16 or float32), cols a multiple of 32, q uint8 [rows, cols / 2].
+ *   Serves activations (a row = a token; STEPS) and weights (a row = an output feature; ROWS) alike.
+ * regione_dequantize_rows_mxfp4: the values that codes and scales stand for, bf16 (every value but those of scale bytes
+ *   253 and 254 above its range fits) or float32.
+ * regione_pack_weight_mxfp4: codes [n, k / 2] and scales [n, k / 32] in rows, k a multiple of 32, to the packed weight of
+ *   regione_packed_weight_mxfp4_bytes(n, k) bytes: k rounded up to 256 with zeros; the codes in blocks of 32 output
+ *   features x 64 inputs (lane l of 64: feature l % 32, the 16 bytes of inputs 32 * (l / 32) on), blocks ordered feature
+ *   block major; behind them the scales of the features (rounded up to 32) in steps.
+ * regione_linear_mxfp4: y[m, n] = act(sum over blocks of 2^(e_x + e_w) sum_i xq wq + b[n]): products exact, sums in
+ *   float32.  xq uint8 [m, k / 2], x_scale in steps; y of out_dtype.  A block of scale 255 makes its row (of a weight:
+ *   its column) NaN. */
+enum { REGIONE_MX_SCALE_ROWS = 0, REGIONE_MX_SCALE_STEPS = 1 };
+int64_t regione_mxfp4_scale_bytes(int64_t rows, int32_t cols, int32_t scale_layout);
+int regione_quantize_rows_mxfp4(regione_ctx* ctx, const void* x, int32_t x_dtype, int64_t rows, int32_t cols, int32_t scale_layout,
+                                void* q, void* scale);
+int regione_dequantize_rows_mxfp4(regione_ctx* ctx, const void* q, const void* scale, int32_t scale_layout, int64_t rows, int32_t cols,
+                                  int32_t out_dtype, void* y);
+int64_t regione_packed_weight_mxfp4_bytes(int32_t n, int32_t k);
+int regione_pack_weight_mxfp4(regione_ctx* ctx, const void* wq, const void* w_scale, int32_t n, int32_t k, void* w_packed);
+int regione_linear_mxfp4(regione_ctx* ctx, const void* xq, const void* x_scale, const void* w_packed, const float* b_opt,
+                         int32_t m, int32_t n, int32_t k, int32_t act, int32_t out_dtype, void* y);
+
+/* Products over groups of rows that have weights of their own, in one launch: the text and image rows of double-stream
+ * blocks (of one or several guidance branches), or rows sorted by expert.  regione_linear and regione_linear_mxfp4 with
+ *   group_offsets [n_groups + 1] int32 on the device, ascending: rows [group_offsets[g], group_offsets[g + 1]) are group g;
+ *   group_weight_opt [n_groups] int32 on the device: which weight group g uses; NULL: weight g;
+ *   w_packed: n_weights packed weights [n, k] one after the other; b_opt [n_weights, n] float32 or NULL.
+ * The host knows neither the groups' sizes nor the number of rows that belong to one; rows of x and y that belong to no
+ * group are neither read nor written.  Offsets outside [0, m] are taken as the nearer end, a group that ends before it
+ * starts is empty, and a group whose weight is not in [0, n_weights) is left out.  At most 65536 groups. */
+int regione_linear_grouped(regione_ctx* ctx, const void* x, const void* w_packed, const float* b_opt, const int32_t* group_offsets,
+                           const int32_t* group_weight_opt, int32_t n_groups, int32_t n_weights, int32_t m, int32_t n, int32_t k,
+                           int32_t act, int32_t out_dtype, void* y);
+int regione_linear_mxfp4_grouped(regione_ctx* ctx, const void* xq, const void* x_scale, const void* w_packed, const float* b_opt,
+                                 const int32_t* group_offsets, const int32_t* group_weight_opt, int32_t n_groups, int32_t n_weights,
+                                 int32_t m, int32_t n, int32_t k, int32_t act, int32_t out_dtype, void* y);
+
 /* One transformer block on the fresh rows: one layer of Phi(tokens, C_KV, f) in
  * Algorithm 1.  The block is LayerNorm (no affine, eps 1e-6) -> modulation -> QKV linear ->
  * attention -> gated residual -> LayerNorm -> modulation -> MLP with tanh-GELU -> gated

@@ -19,6 +19,7 @@ BF16, FP32 = 0, 1
 BLOCK_DOUBLE, BLOCK_SINGLE = 0, 1
 FLAG_STORE, FLAG_RETRIEVE = 1, 2
 ACT_NONE, ACT_GELU_TANH, ACT_SILU = 0, 1, 2
+MX_SCALE_ROWS, MX_SCALE_STEPS = 0, 1
 
 EXPORTS = (
     "regione_last_error", "regione_create", "regione_destroy", "regione_partition", "regione_gather",
@@ -33,6 +34,8 @@ EXPORTS = (
     "regione_euler_rows", "regione_gather_pair", "regione_scatter_pair", "regione_velocity_head", "regione_region_step",
     "regione_block_forward_fp8", "regione_gemm_plan_host", "regione_block_lanes_host",
     "regione_tune_attention_form", "regione_attention_workgroups",
+    "regione_mxfp4_scale_bytes", "regione_quantize_rows_mxfp4", "regione_dequantize_rows_mxfp4", "regione_packed_weight_mxfp4_bytes",
+    "regione_pack_weight_mxfp4", "regione_linear_mxfp4", "regione_linear_grouped", "regione_linear_mxfp4_grouped",
 )
 STEP_FULL, STEP_FULL_STORE, STEP_REGION = 0, 1, 2
 PROF_NAMES = ("partition", "rows", "layernorm", "gemm", "attention", "velocity")
@@ -151,6 +154,14 @@ def lib() -> C.CDLL:
             "regione_quantize_rows_fp8": [vp, vp, i64, i32, vp, vp],
             "regione_pack_weight_fp8": [vp, vp, i32, i32, vp],
             "regione_linear_fp8": [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp],
+            "regione_mxfp4_scale_bytes": [i64, i32, i32],
+            "regione_quantize_rows_mxfp4": [vp, vp, i32, i64, i32, i32, vp, vp],
+            "regione_dequantize_rows_mxfp4": [vp, vp, vp, i32, i64, i32, i32, vp],
+            "regione_packed_weight_mxfp4_bytes": [i32, i32],
+            "regione_pack_weight_mxfp4": [vp, vp, vp, i32, i32, vp],
+            "regione_linear_mxfp4": [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp],
+            "regione_linear_grouped": [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp],
+            "regione_linear_mxfp4_grouped": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp],
             "regione_tune_gemm": [vp, i32, i32],
             "regione_block_lanes_host": [i32, i32, i32, i32, i32, C.POINTER(i32)],
             "regione_tune_attention": [vp, i32],
@@ -173,6 +184,7 @@ def lib() -> C.CDLL:
             fn.restype = C.c_int
         _lib.regione_packed_weight_elems.argtypes = [i32, i32]
         _lib.regione_packed_weight_elems.restype = C.c_int64
+        _lib.regione_mxfp4_scale_bytes.restype = _lib.regione_packed_weight_mxfp4_bytes.restype = C.c_int64
     return _lib
 
 
@@ -499,6 +511,60 @@ def regione_pack_weight_fp8(ctx, wq, n, k, wq_packed):
 
 def regione_linear_fp8(ctx, xq, x_scale, wq_packed, w_scale, b, m, n, k, act, out_dtype, y):
     _check(lib().regione_linear_fp8(ctx.handle, _p(xq), _p(x_scale), _p(wq_packed), _p(w_scale), _p(b), m, n, k, act, out_dtype, _p(y)))
+
+
+def regione_mxfp4_scale_bytes(rows: int, cols: int, layout: int) -> int:
+    return int(lib().regione_mxfp4_scale_bytes(rows, cols, layout))
+
+
+def regione_quantize_rows_mxfp4(ctx, x, x_dtype, rows, cols, layout, q, scale):
+    _check(lib().regione_quantize_rows_mxfp4(ctx.handle, _p(x), x_dtype, rows, cols, layout, _p(q), _p(scale)))
+
+
+def regione_dequantize_rows_mxfp4(ctx, q, scale, layout, rows, cols, out_dtype, y):
+    _check(lib().regione_dequantize_rows_mxfp4(ctx.handle, _p(q), _p(scale), layout, rows, cols, out_dtype, _p(y)))
+
+
+def regione_packed_weight_mxfp4_bytes(n: int, k: int) -> int:
+    return int(lib().regione_packed_weight_mxfp4_bytes(n, k))
+
+
+def regione_pack_weight_mxfp4(ctx, wq, w_scale, n, k, w_packed):
+    _check(lib().regione_pack_weight_mxfp4(ctx.handle, _p(wq), _p(w_scale), n, k, _p(w_packed)))
+
+
+def regione_linear_mxfp4(ctx, xq, x_scale, w_packed, b, m, n, k, act, out_dtype, y):
+    _check(lib().regione_linear_mxfp4(ctx.handle, _p(xq), _p(x_scale), _p(w_packed), _p(b), m, n, k, act, out_dtype, _p(y)))
+
+
+def regione_linear_grouped(ctx, x, w_packed, b, group_offsets, group_weight, n_groups, n_weights, m, n, k, act, out_dtype, y):
+    _check(lib().regione_linear_grouped(ctx.handle, _p(x), _p(w_packed), _p(b), _p(group_offsets), _p(group_weight), n_groups, n_weights,
+                                        m, n, k, act, out_dtype, _p(y)))
+
+
+def regione_linear_mxfp4_grouped(ctx, xq, x_scale, w_packed, b, group_offsets, group_weight, n_groups, n_weights, m, n, k, act, out_dtype, y):
+    _check(lib().regione_linear_mxfp4_grouped(ctx.handle, _p(xq), _p(x_scale), _p(w_packed), _p(b), _p(group_offsets), _p(group_weight), n_groups, n_weights,
+                                              m, n, k, act, out_dtype, _p(y)))
+
+
+def quantize_rows_mxfp4(ctx, x, layout: int = MX_SCALE_STEPS):
+    """Convenience: (codes, scale bytes) of a CUDA tensor [rows, cols], bf16 or float32, as new tensors."""
+    import torch
+    rows, cols = x.shape
+    q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device)
+    scale = torch.empty(regione_mxfp4_scale_bytes(rows, cols, layout), dtype=torch.uint8, device=x.device)
+    regione_quantize_rows_mxfp4(ctx, x.contiguous(), FP32 if x.dtype == torch.float32 else BF16, rows, cols, layout, q, scale)
+    return q, scale
+
+
+def pack_weight_mxfp4(ctx, w):
+    """Convenience: quantises a row-major CUDA tensor [n, k], bf16 or float32, and packs it into a new tensor in the library's layout."""
+    import torch
+    n, k = w.shape
+    q, scale = quantize_rows_mxfp4(ctx, w, MX_SCALE_ROWS)
+    out = torch.empty(regione_packed_weight_mxfp4_bytes(n, k), dtype=torch.uint8, device=w.device)
+    regione_pack_weight_mxfp4(ctx, q, scale, n, k, out)
+    return out
 
 
 def regione_tune_gemm(ctx, wave_tile_blocks: int, k_splits: int):
