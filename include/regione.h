@@ -251,7 +251,7 @@ int regione_linear_fp8(regione_ctx* ctx, const void* xq, const float* x_scale, c
  * Scales lie in one of two layouts:
  *   REGIONE_MX_SCALE_ROWS  [rows, cols / 32] bytes, as the specification's tensors are usually kept;
  *   REGIONE_MX_SCALE_STEPS what the products read: for every step of 256 columns, the rows (rounded up to an even
- *     number) of eight bytes; block b of a step at byte 2 * (b % 4) + b / 4; blocks past the row's end are zero (the
+ *     number) of eight bytes; block b of a step at byte 4 * (b % 2) + b / 2; blocks past the row's end are zero (the
  *     quantiser writes them).
  * regione_mxfp4_scale_bytes gives the size of either.
  *

@@ -65,13 +65,13 @@ def unpack_codes(q) -> np.ndarray:
 
 
 def scale_steps(scale) -> np.ndarray:
-    """Scale bytes [rows, blocks] in the layout of steps: [steps, rows rounded up to even, 8], block b of a step at byte 2 (b % 4) + b / 4.  Bytes of rows that
+    """Scale bytes [rows, blocks] in the layout of steps: [steps, rows rounded up to even, 8], block b of a step at byte 4 (b % 2) + b / 2.  Bytes of rows that
     do not exist are zero here and may be anything."""
     rows, blocks = np.asarray(scale).shape
     steps = -(-blocks // 8)
     out = np.zeros((steps, (rows + 1) // 2 * 2, 8), dtype=np.uint8)
     for b in range(blocks):
-        out[b // 8, :rows, 2 * (b % 8 % 4) + b % 8 // 4] = scale[:, b]
+        out[b // 8, :rows, 4 * (b % 2) + b % 8 // 2] = scale[:, b]
     return out
 
 

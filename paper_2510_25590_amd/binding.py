@@ -35,7 +35,7 @@ EXPORTS = (
     "regione_block_forward_fp8", "regione_gemm_plan_host", "regione_block_lanes_host",
     "regione_tune_attention_form", "regione_attention_workgroups",
     "regione_mxfp4_scale_bytes", "regione_quantize_rows_mxfp4", "regione_dequantize_rows_mxfp4", "regione_packed_weight_mxfp4_bytes",
-    "regione_pack_weight_mxfp4", "regione_linear_mxfp4", "regione_linear_grouped", "regione_linear_mxfp4_grouped",
+    "regione_pack_weight_mxfp4", "regione_linear_mxfp4", "regione_linear_grouped", "regione_linear_mxfp4_grouped", "regione_tune_mx",
 )
 STEP_FULL, STEP_FULL_STORE, STEP_REGION = 0, 1, 2
 PROF_NAMES = ("partition", "rows", "layernorm", "gemm", "attention", "velocity")
@@ -161,6 +161,7 @@ def lib() -> C.CDLL:
             "regione_pack_weight_mxfp4": [vp, vp, vp, i32, i32, vp],
             "regione_linear_mxfp4": [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp],
             "regione_linear_grouped": [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp],
+            "regione_tune_mx": [vp, i32, i32],
             "regione_linear_mxfp4_grouped": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp],
             "regione_tune_gemm": [vp, i32, i32],
             "regione_block_lanes_host": [i32, i32, i32, i32, i32, C.POINTER(i32)],
@@ -545,6 +546,10 @@ def regione_linear_grouped(ctx, x, w_packed, b, group_offsets, group_weight, n_g
 def regione_linear_mxfp4_grouped(ctx, xq, x_scale, w_packed, b, group_offsets, group_weight, n_groups, n_weights, m, n, k, act, out_dtype, y):
     _check(lib().regione_linear_mxfp4_grouped(ctx.handle, _p(xq), _p(x_scale), _p(w_packed), _p(b), _p(group_offsets), _p(group_weight), n_groups, n_weights,
                                               m, n, k, act, out_dtype, _p(y)))
+
+
+def regione_tune_mx(ctx, tile: int, k_splits: int = 0):
+    _check(lib().regione_tune_mx(ctx.handle, tile, k_splits))
 
 
 def quantize_rows_mxfp4(ctx, x, layout: int = MX_SCALE_STEPS):

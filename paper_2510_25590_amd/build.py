@@ -15,10 +15,10 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libregione.so")
 SOURCES = ["api.hip", "partition.hip", "rows.hip", "gemm.hip", "gemm_tiles_wide.hip", "gemm_tiles_128.hip", "gemm_tiles_96.hip", "gemm_tiles_kg.hip", "gemm_tiles_fp8.hip",
-           "attention.hip", "block_extras.hip", "fp8.hip", "mxfp4.hip", "gemm_mx.hip", "peaks.hip", "fp32.hip", "host_logic.cpp"]
+           "attention.hip", "block_extras.hip", "fp8.hip", "mxfp4.hip", "gemm_mx.hip", "gemm_mx_tiles_4bit.hip", "gemm_mx_tiles_bf16.hip", "peaks.hip", "fp32.hip", "host_logic.cpp"]
 
 # sources whose machine code is checked, and by which function of isa_check.py
-CHECKED = {**dict.fromkeys(("gemm.hip", "gemm_tiles_wide.hip", "gemm_tiles_128.hip", "gemm_tiles_96.hip", "gemm_tiles_kg.hip", "gemm_tiles_fp8.hip", "gemm_mx.hip"), "check_asm"),
+CHECKED = {**dict.fromkeys(("gemm.hip", "gemm_tiles_wide.hip", "gemm_tiles_128.hip", "gemm_tiles_96.hip", "gemm_tiles_kg.hip", "gemm_tiles_fp8.hip", "gemm_mx.hip", "gemm_mx_tiles_4bit.hip", "gemm_mx_tiles_bf16.hip"), "check_asm"),
            "attention.hip": "check_attention_asm"}
 
 

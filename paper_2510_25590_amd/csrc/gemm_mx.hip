@@ -3,16 +3,28 @@
 
 namespace {
 
-int launch(regione_ctx* ctx, int fmt, const MxOperands& p, const GemmEpilogue& ep) {
-    ProfScope prof(ctx, REGIONE_PROF_GEMM);
-    const int64_t row_tiles = (static_cast<int64_t>(p.m) + kMxSmallRows - 1) / kMxSmallRows + (p.offsets ? (p.n_groups < p.m ? p.n_groups : p.m) : 0);
-    const int64_t tiles = row_tiles * ((p.n + 31) / 32);
-    if (tiles >= int64_t(1) << 23) RG_FAIL(REGIONE_ERR_UNSUPPORTED, "linear: a result of %d x %d", p.m, p.n);    // 2^32 threads
-    const dim3 grid(static_cast<unsigned>(tiles));
-    if (fmt == MX_FP4) hipLaunchKernelGGL((gemm_mx_small_kernel<MX_FP4, 2>), grid, dim3(kMxSmallWaves * 64), 0, ctx->stream, p, ep);
-    else hipLaunchKernelGGL((gemm_mx_small_kernel<MX_BF16, 2>), grid, dim3(kMxSmallWaves * 64), 0, ctx->stream, p, ep);
+template <int FMT, int CF>
+int launch_small(regione_ctx* ctx, const MxOperands& p, const GemmEpilogue& ep) {
+    const int64_t tiles = mx_most_row_tiles(p, kMxSmallRows) * ((p.n + 16 * CF - 1) / (16 * CF));
+    if (tiles >= (int64_t{1} << 32) / (kMxSmallWaves * 64)) RG_FAIL(REGIONE_ERR_UNSUPPORTED, "linear: a result of %d x %d", p.m, p.n);
+    hipLaunchKernelGGL((gemm_mx_small_kernel<FMT, CF>), dim3(static_cast<unsigned>(tiles)), dim3(kMxSmallWaves * 64), 0, ctx->stream, p, ep);
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
+}
+
+struct MxPlan { int tile, splits; };      // tile 1: the kernel of 16 rows
+
+MxPlan choose(const MxOperands& p) {
+    if (p.m <= 64) return {1, 1};
+    return {44, 1};
+}
+
+int launch(regione_ctx* ctx, int fmt, const MxOperands& p, const GemmEpilogue& ep) {
+    ProfScope prof(ctx, REGIONE_PROF_GEMM);
+    MxPlan plan = choose(p);
+    if (ctx->mx_force_tile) plan = {ctx->mx_force_tile, ctx->mx_force_splits > 0 && !p.offsets ? ctx->mx_force_splits : 1};
+    if (plan.tile == 1) return fmt == MX_FP4 ? launch_small<MX_FP4, 2>(ctx, p, ep) : launch_small<MX_BF16, 2>(ctx, p, ep);
+    return fmt == MX_FP4 ? rg_mx_tile_4bit(ctx, plan.tile, p, plan.splits, ep) : rg_mx_tile_bf16(ctx, plan.tile, p, plan.splits, ep);
 }
 
 // What the three products have in common.  groups: offsets, use, n_groups and n_weights are looked at.
@@ -58,4 +70,14 @@ extern "C" int regione_linear_mxfp4_grouped(regione_ctx* ctx, const void* xq, co
 extern "C" int regione_linear_grouped(regione_ctx* ctx, const void* x, const void* w_packed, const float* b_opt, const int32_t* group_offsets,
                                       const int32_t* group_weight_opt, int32_t n_groups, int32_t n_weights, int32_t m, int32_t n, int32_t k, int32_t act, int32_t out_dtype, void* y) {
     return linear(ctx, "linear_grouped", MX_BF16, true, x, nullptr, w_packed, b_opt, group_offsets, group_weight_opt, n_groups, n_weights, m, n, k, act, out_dtype, y);
+}
+
+extern "C" int regione_tune_mx(regione_ctx* ctx, int32_t tile, int32_t k_splits) {
+    if (!ctx) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: null context");
+    bool known = tile == 0 || tile == 1;
+    for (int t : {44, 34, 24, 42, 22, 12, 21, 11}) known = known || t == tile;
+    if (!known || k_splits < 0 || k_splits > 16) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: no tile %d, or k_splits=%d is not in 0..16", tile, k_splits);
+    ctx->mx_force_tile = tile;
+    ctx->mx_force_splits = k_splits;
+    return REGIONE_OK;
 }

@@ -58,7 +58,7 @@ def test_step_layout(rows, blocks):
     assert len(flat) == -(-blocks // 8) * padded * 8
     for r in range(rows):
         for b in range(blocks):
-            assert flat[(b // 8 * padded + r) * 8 + 2 * (b % 4) + (b % 8 >= 4)] == scale[r, b]
+            assert flat[(b // 8 * padded + r) * 8 + 4 * (b % 2) + b % 8 // 2] == scale[r, b]
 
 
 def test_groups_by_hand():
