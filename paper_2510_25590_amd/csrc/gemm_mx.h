@@ -33,37 +33,39 @@ __device__ __forceinline__ MxGroupLane mx_group_lane(const MxOperands& p, int g)
     return t;
 }
 __device__ __forceinline__ int mx_prefix(int v) {              // sum over the lanes up to this one
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int other = __shfl_up(v, d);
-        if ((threadIdx.x & 63) >= static_cast<unsigned>(d)) v += other;
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);      // within rows of 16: from one, two, four and eight lanes below
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);     // the first row's last lane to the second row, the third's to the fourth
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // the second row's last lane to both above
+}
+// Row tiles of a launch: of all rows, or of all groups.  The first 64 groups stay in the lanes.
+template <int R> struct MxTiles {
+    MxGroupLane lane;
+    int upto, total;
+    __device__ __forceinline__ explicit MxTiles(const MxOperands& p) {
+        if (!p.offsets) { total = (p.m + R - 1) / R; return; }
+        lane = mx_group_lane<R>(p, threadIdx.x & 63);
+        upto = mx_prefix(lane.tiles);
+        total = __builtin_amdgcn_readlane(upto, 63);
+        for (int g0 = 64; g0 < p.n_groups; g0 += 64) total += __builtin_amdgcn_readlane(mx_prefix(mx_group_lane<R>(p, g0 + (threadIdx.x & 63)).tiles), 63);
     }
-    return v;
-}
-// Row tiles of a launch: of all rows, or of all groups.
-template <int R>
-__device__ __forceinline__ int mx_row_tiles(const MxOperands& p) {
-    if (!p.offsets) return (p.m + R - 1) / R;
-    int total = 0;
-    for (int g0 = 0; g0 < p.n_groups; g0 += 64) total += __builtin_amdgcn_readlane(mx_prefix(mx_group_lane<R>(p, g0 + (threadIdx.x & 63)).tiles), 63);
-    return total;
-}
-// Row tile `unit` of them.
-template <int R>
-__device__ __forceinline__ MxTile mx_find_tile(const MxOperands& p, int unit) {
-    if (!p.offsets) return {unit * R, 0, p.m, 0};
-    int before = 0;
-    for (int g0 = 0; ; g0 += 64) {
-        const MxGroupLane t = mx_group_lane<R>(p, g0 + (threadIdx.x & 63));
-        const int upto = mx_prefix(t.tiles), total = __builtin_amdgcn_readlane(upto, 63);
-        if (unit < before + total) {
-            const int at = __builtin_ctzll(__ballot(before + upto > unit));          // the group that holds the unit
-            const int row0 = __builtin_amdgcn_readlane(t.first, at) + (unit - before - __builtin_amdgcn_readlane(upto - t.tiles, at)) * R;
-            return {row0, __builtin_amdgcn_readlane(t.lo, at), __builtin_amdgcn_readlane(t.hi, at), __builtin_amdgcn_readlane(t.weight, at)};
+    __device__ __forceinline__ MxTile find(const MxOperands& p, int unit) const {
+        if (!p.offsets) return {unit * R, 0, p.m, 0};
+        MxGroupLane t = lane;
+        int sum = upto, before = 0, here = __builtin_amdgcn_readlane(upto, 63);
+        for (int g0 = 64; unit >= before + here; g0 += 64) {
+            before += here;
+            t = mx_group_lane<R>(p, g0 + (threadIdx.x & 63));
+            sum = mx_prefix(t.tiles);
+            here = __builtin_amdgcn_readlane(sum, 63);
         }
-        before += total;
+        const int at = __builtin_ctzll(__ballot(before + sum > unit));           // the group that holds the unit
+        const int row0 = __builtin_amdgcn_readlane(t.first, at) + (unit - before - __builtin_amdgcn_readlane(sum - t.tiles, at)) * R;
+        return {row0, __builtin_amdgcn_readlane(t.lo, at), __builtin_amdgcn_readlane(t.hi, at), __builtin_amdgcn_readlane(t.weight, at)};
     }
-}
+};
 
 __device__ __forceinline__ i32x8 mx_half_operand(const u32x4& v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
 // One 16x16 instruction on half H of a step; a lane's scales of the two halves are bytes 0 and 2 (block l/16 of the half, see mx_scale_step).
@@ -73,36 +75,32 @@ __device__ __forceinline__ f32x4 mx_mfma(const u32x4& w, const u32x4& a, const f
     else return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_half_operand(w), mx_half_operand(a), acc, 4, 4, 2 * H, static_cast<int>(w_scale), 2 * H, static_cast<int>(a_scale));
 }
 
-// 16 rows x 16*CF columns per workgroup; its waves split K, read their fragments straight from memory with the loads of CHUNK steps in flight, and meet in LDS,
-// where the sums are formed in wave order.
+// Few rows: a wave owns 16 rows x 32 columns of a part of K and reads its operands straight from memory, the weights as they lie, with the loads of CHUNK steps in flight.  KW of a workgroup's
+// eight waves share K and meet in LDS, where the sums are formed in wave order; the others take further columns.  Such a launch is a chain of trips to memory and the reading of
+// the weights.
 constexpr int kMxSmallRows = 16, kMxSmallWaves = 8;
 
-template <int FMT, int CF>
-__global__ void __launch_bounds__(kMxSmallWaves * 64) __attribute__((amdgpu_waves_per_eu(2)))
+template <int FMT, int KW>
+__global__ void __launch_bounds__(kMxSmallWaves * 64) __attribute__((amdgpu_waves_per_eu(4)))
 gemm_mx_small_kernel(MxOperands p, GemmEpilogue ep) {
-    constexpr int CHUNK = CF == 2 ? 6 : 3;
-    __shared__ __attribute__((aligned(16))) f32x4 sums[kMxSmallWaves * CF * 64];
-    const int n_tiles = (p.n + 16 * CF - 1) / (16 * CF), unit = static_cast<int>(blockIdx.x) / n_tiles;
-    if (unit >= mx_row_tiles<kMxSmallRows>(p)) return;
-    const MxTile t = mx_find_tile<kMxSmallRows>(p, unit);
+    constexpr int CF = 2, CHUNK = FMT == MX_FP4 ? 2 : 3, NW = kMxSmallWaves / KW;
+    __shared__ __attribute__((aligned(16))) f32x4 sums[KW == 1 ? 1 : kMxSmallWaves * CF * 64];
+    const int n_tiles = (p.n + 32 * NW - 1) / (32 * NW), unit = static_cast<int>(blockIdx.x) / n_tiles;
+    const MxTiles<kMxSmallRows> tiles(p);
+    if (unit >= tiles.total) return;
+    const MxTile t = tiles.find(p, unit);
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kw = wave % KW;
     const int l16 = lane & 15, kc = lane >> 4;
-    const int n0 = (static_cast<int>(blockIdx.x) - unit * n_tiles) * (16 * CF), n32 = (p.n + 31) & ~31;
-    const int per = (p.steps + kMxSmallWaves - 1) / kMxSmallWaves, s0 = wave * per, s1 = s0 + per < p.steps ? s0 + per : p.steps;
+    const int n0 = ((static_cast<int>(blockIdx.x) - unit * n_tiles) * NW + wave / KW) * 32, n32 = (p.n + 31) & ~31;
+    const int per = (p.steps + KW - 1) / KW, s0 = kw * per, s1 = s0 + per < p.steps ? s0 + per : p.steps;
 
     const uint8_t* w = p.w + t.weight * p.w_stride;
-    const uint8_t* wp[CF / 2];
-    const uint8_t* wsp[CF];
-#pragma unroll
-    for (int b = 0; b < CF / 2; ++b) {
-        int nb = (n0 >> 5) + b;
-        nb = nb < n32 / 32 ? nb : n32 / 32 - 1;                 // blocks past N repeat the last one; their sums are not stored
-        const int col = 8 * (l16 >> 2) + (l16 & 3);             // of fragment 2 b; the other one's is four further (see gemm_epilogue16)
-        wp[b] = w + ((static_cast<int64_t>(nb) * p.steps * 4 + (kc >> 1)) * 64 + (kc & 1) * 32 + col) * 16;
-#pragma unroll
-        for (int jl = 0; jl < 2; ++jl) wsp[2 * b + jl] = w + static_cast<int64_t>(n32) * p.steps * 128 + (nb * 32 + col + 4 * jl) * 8 + 4 * (kc & 1);
-    }
+    int nb = n0 >> 5;
+    nb = nb < n32 / 32 ? nb : n32 / 32 - 1;                     // blocks past N repeat the last one; their sums are not stored
+    const int col0 = 8 * (l16 >> 2) + (l16 & 3);                // of the first fragment; the other one's is four further (see gemm_epilogue16)
+    const uint8_t* wp = w + ((static_cast<int64_t>(nb) * p.steps * 4 + (kc >> 1)) * 64 + (kc & 1) * 32 + col0) * 16;
+    const uint8_t* wsp = w + static_cast<int64_t>(n32) * p.steps * 128 + (nb * 32 + col0) * 8 + 4 * (kc & 1);
     int row = t.row0 + l16;
     row = row < t.end ? row : t.end - 1;                        // rows past the end repeat the last one
     const uint8_t* ap = p.a + static_cast<int64_t>(row) * p.row_bytes;
@@ -122,49 +120,48 @@ gemm_mx_small_kernel(MxOperands p, GemmEpilogue ep) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int at = s * 128 + h * 64 + kc * 16;  // past the row's end the weights are zero, and a row's first values serve
-                    av[i][h] = *reinterpret_cast<const u32x4*>(ap + (at < p.row_bytes ? at : 0));
 #pragma unroll
-                    for (int j = 0; j < CF; ++j)
-                        wv[i][h][j] = *reinterpret_cast<const u32x4*>(wp[j >> 1] + (static_cast<int64_t>(s) * 4 + 2 * h) * 1024 + (j & 1) * 64);
+                    for (int j = 0; j < CF; ++j) wv[i][h][j] = *reinterpret_cast<const u32x4*>(wp + (static_cast<int64_t>(s) * 4 + 2 * h) * 1024 + j * 64);
+                    av[i][h] = *reinterpret_cast<const u32x4*>(ap + (at < p.row_bytes ? at : 0));
                 }
                 if (FMT == MX_FP4) {
-                    as[i] = *reinterpret_cast<const unsigned*>(asp + s * a_step) >> (8 * (kc >> 1));
 #pragma unroll
-                    for (int j = 0; j < CF; ++j) ws[i][j] = *reinterpret_cast<const unsigned*>(wsp[j] + static_cast<int64_t>(s) * n32 * 8) >> (8 * (kc >> 1));
+                    for (int j = 0; j < CF; ++j) ws[i][j] = *reinterpret_cast<const unsigned*>(wsp + static_cast<int64_t>(s) * n32 * 8 + j * 32);
+                    as[i] = *reinterpret_cast<const unsigned*>(asp + s * a_step);
                 }
             }
         }
 #pragma unroll
         for (int i = 0; i < CHUNK; ++i)
             if (base + i < s1) {
+                const unsigned shift = 8 * (kc >> 1);
 #pragma unroll
-                for (int j = 0; j < CF; ++j) acc[j] = mx_mfma<FMT, 0>(wv[i][0][j], av[i][0], acc[j], ws[i][j], as[i]);
+                for (int j = 0; j < CF; ++j) acc[j] = mx_mfma<FMT, 0>(wv[i][0][j], av[i][0], acc[j], ws[i][j] >> shift, as[i] >> shift);
 #pragma unroll
-                for (int j = 0; j < CF; ++j) acc[j] = mx_mfma<FMT, 1>(wv[i][1][j], av[i][1], acc[j], ws[i][j], as[i]);
+                for (int j = 0; j < CF; ++j) acc[j] = mx_mfma<FMT, 1>(wv[i][1][j], av[i][1], acc[j], ws[i][j] >> shift, as[i] >> shift);
             }
     }
+    if (KW > 1) {
 #pragma unroll
-    for (int j = 0; j < CF; ++j) sums[(wave * CF + j) * 64 + lane] = acc[j];
-    __syncthreads();
-    if (wave >= CF / 2) return;
-    f32x4 sum[2];
+        for (int j = 0; j < CF; ++j) sums[(wave * CF + j) * 64 + lane] = acc[j];
+        __syncthreads();
+        if (kw) return;
 #pragma unroll
-    for (int jl = 0; jl < 2; ++jl) {
-        sum[jl] = sums[(2 * wave + jl) * 64 + lane];
+        for (int v = 1; v < KW; ++v)
 #pragma unroll
-        for (int v = 1; v < kMxSmallWaves; ++v) sum[jl] += sums[(v * CF + 2 * wave + jl) * 64 + lane];
+            for (int j = 0; j < CF; ++j) acc[j] += sums[((wave + v) * CF + j) * 64 + lane];
     }
     if (ep.bias) ep.bias += static_cast<int64_t>(t.weight) * p.n;
-    const int col = n0 + 32 * wave + 8 * kc;
+    const int col = n0 + 8 * kc;
     if (t.row0 + l16 >= t.end || t.row0 + l16 < t.begin || col >= p.n) return;
-    if (col + 8 > p.n) { epilogue_ragged<EPI_PLAIN, false>(ep, row, col, p.n, sum[0], sum[1]); return; }
+    if (col + 8 > p.n) { epilogue_ragged<EPI_PLAIN, false>(ep, row, col, p.n, acc[0], acc[1]); return; }
     EpiColumns<EPI_PLAIN, false> cols;
     EpiRow<EPI_PLAIN, false> r;
     Raw8 raw;
     cols.load(ep, col);
     r.load(ep, row);
-    if (ep.vec_ok) epilogue_store8<EPI_PLAIN, false, true>(ep, row, col, sum[0], sum[1], cols, r, raw);
-    else epilogue_store8<EPI_PLAIN, false, false>(ep, row, col, sum[0], sum[1], cols, r, raw);
+    if (ep.vec_ok) epilogue_store8<EPI_PLAIN, false, true>(ep, row, col, acc[0], acc[1], cols, r, raw);
+    else epilogue_store8<EPI_PLAIN, false, false>(ep, row, col, acc[0], acc[1], cols, r, raw);
 }
 
 }  // namespace

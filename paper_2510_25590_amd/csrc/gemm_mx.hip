@@ -3,19 +3,24 @@
 
 namespace {
 
-template <int FMT, int CF>
+template <int FMT, int KW>
 int launch_small(regione_ctx* ctx, const MxOperands& p, const GemmEpilogue& ep) {
-    const int64_t tiles = mx_most_row_tiles(p, kMxSmallRows) * ((p.n + 16 * CF - 1) / (16 * CF));
+    constexpr int COLS = 32 * kMxSmallWaves / KW;
+    const int64_t tiles = mx_most_row_tiles(p, kMxSmallRows) * ((p.n + COLS - 1) / COLS);
     if (tiles >= (int64_t{1} << 32) / (kMxSmallWaves * 64)) RG_FAIL(REGIONE_ERR_UNSUPPORTED, "linear: a result of %d x %d", p.m, p.n);
-    hipLaunchKernelGGL((gemm_mx_small_kernel<FMT, CF>), dim3(static_cast<unsigned>(tiles)), dim3(kMxSmallWaves * 64), 0, ctx->stream, p, ep);
+    hipLaunchKernelGGL((gemm_mx_small_kernel<FMT, KW>), dim3(static_cast<unsigned>(tiles)), dim3(kMxSmallWaves * 64), 0, ctx->stream, p, ep);
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }
+template <int FMT>
+int launch_small(regione_ctx* ctx, int waves, const MxOperands& p, const GemmEpilogue& ep) {
+    return waves == 1 ? launch_small<FMT, 1>(ctx, p, ep) : waves == 2 ? launch_small<FMT, 2>(ctx, p, ep) : waves == 4 ? launch_small<FMT, 4>(ctx, p, ep) : launch_small<FMT, 8>(ctx, p, ep);
+}
 
-struct MxPlan { int tile, splits; };      // tile 1: the kernel of 16 rows
+struct MxPlan { int tile, splits; };      // tile 1, 2, 4, 8: the kernel of 16 rows with as many waves over K
 
 MxPlan choose(const MxOperands& p) {
-    if (p.m <= 64) return {1, 1};
+    if (p.m <= 64) return {8, 1};
     return {44, 1};
 }
 
@@ -23,7 +28,7 @@ int launch(regione_ctx* ctx, int fmt, const MxOperands& p, const GemmEpilogue& e
     ProfScope prof(ctx, REGIONE_PROF_GEMM);
     MxPlan plan = choose(p);
     if (ctx->mx_force_tile) plan = {ctx->mx_force_tile, ctx->mx_force_splits > 0 && !p.offsets ? ctx->mx_force_splits : 1};
-    if (plan.tile == 1) return fmt == MX_FP4 ? launch_small<MX_FP4, 2>(ctx, p, ep) : launch_small<MX_BF16, 2>(ctx, p, ep);
+    if (plan.tile <= 8) return fmt == MX_FP4 ? launch_small<MX_FP4>(ctx, plan.tile, p, ep) : launch_small<MX_BF16>(ctx, plan.tile, p, ep);
     return fmt == MX_FP4 ? rg_mx_tile_4bit(ctx, plan.tile, p, plan.splits, ep) : rg_mx_tile_bf16(ctx, plan.tile, p, plan.splits, ep);
 }
 
@@ -74,8 +79,8 @@ extern "C" int regione_linear_grouped(regione_ctx* ctx, const void* x, const voi
 
 extern "C" int regione_tune_mx(regione_ctx* ctx, int32_t tile, int32_t k_splits) {
     if (!ctx) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: null context");
-    bool known = tile == 0 || tile == 1;
-    for (int t : {44, 34, 24, 42, 22, 12, 21, 11}) known = known || t == tile;
+    bool known = tile == 0;
+    for (int t : {1, 2, 4, 8, 44, 324, 342, 322, 34, 24, 42, 22, 12, 21, 11}) known = known || t == tile;
     if (!known || k_splits < 0 || k_splits > 16) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: no tile %d, or k_splits=%d is not in 0..16", tile, k_splits);
     ctx->mx_force_tile = tile;
     ctx->mx_force_splits = k_splits;

@@ -4,7 +4,7 @@
 // feed 16 instructions of 32 cycles, half of what the LDS delivers in that time (a quarter more goes into the copies).  The 32x32 instruction reaches its rate with one
 // wave per SIMD, which the 16x16 one does not (register-only loops in 4 bits, PFLOP/s with one, two and four waves per SIMD: 6.3 / 6.5 / 6.6 against 4.2 / 5.5 / 6.1).
 //
-// K goes by in half steps (64 bytes of every row), copied from global memory straight into a ring of four LDS slots; a half step is two phases of RF * CF instructions.
+// K goes by in half steps (64 bytes of every row), copied from global memory straight into a ring of three or four LDS slots; a half step is two phases of RF * CF instructions.
 // While a phase's instructions run, the same wave reads the operands of the next phase and issues a share of the copies; one barrier per half step.
 #pragma once
 #include "gemm_mx.h"
@@ -25,14 +25,15 @@ __device__ __forceinline__ uint64_t mx_lanes_if(int a, int b) {
     return lanes;
 }
 
-template <int FMT, int RF, int CF> struct MxTileShape {
-    static constexpr int ROWS = 64 * RF, COLS = 64 * CF, THREADS = 256, SLOTS = 4;
+template <int FMT, int RF, int CF, int SLOTS> struct MxTileShape {
+    static constexpr int ROWS = 64 * RF, COLS = 64 * CF, THREADS = 256;
     static constexpr int COPIES = RF + CF;                          // 1 KiB copies per wave and half step: RF of 16 rows, CF of a weight block's 64 inputs
     static constexpr unsigned SLOT = (ROWS + COLS) * 64u, W_BASE = ROWS * 64u;
     static constexpr unsigned SCALES = FMT == MX_FP4 ? (ROWS + COLS) * 8u : 0u, S_BASE = SLOTS * SLOT;      // of a whole step; two of them
     static constexpr unsigned LDS_BYTES = S_BASE + 2 * SCALES;
     static constexpr int STORE_ROWS = RF % 2 == 0 && 2 * CF * 16384u <= LDS_BYTES ? 2 : 1;                   // rows of fragments per wave that mx_store leaves in LDS at a time
     static_assert(STORE_ROWS * CF * 16384u <= LDS_BYTES, "four waves' fragments");
+    static constexpr int FIT = 163840 / LDS_BYTES, WAVES = RF * CF > 8 ? 1 : FIT < 2 ? 2 : FIT > 4 ? 4 : FIT;    // workgroups that a CU's LDS holds; waves per SIMD that registers are kept for
     static constexpr int64_t PART_FLOATS = static_cast<int64_t>(ROWS) * COLS;
 };
 
@@ -52,7 +53,7 @@ template <bool ACC_REGISTERS> __device__ __forceinline__ f32x16 mx_here(f32x16 v
 
 // Writes a wave's accumulators: acc[i][j] of a lane holds row 32*i + lane%32 and columns 32*j + 16*b + 8*(lane/32) + 0..7, b = 0, 1, of the wave's part.  By way of LDS (the wave's own
 // part of it, IR rows of fragments at a time), so that a store covers whole rows of the part, 256 bytes at 128 bf16 columns: straight from the accumulators, 32 bytes of 32
-// rows at a time, 2048 x 8192 x 256 took MXT_DIRECT us instead of MXT_LDS.
+// rows at a time, 2048 x 8192 x 256 took 17.6 us instead of 15.1.
 template <int RF, int CF, int IR, bool ALIGNED>
 __device__ __forceinline__ void mx_store(const f32x16 (&acc)[RF][CF], unsigned char* lds, const MxTile& t, int N, int m0, int n0w, const GemmEpilogue& ep) {
     constexpr int PIECES = 8 * CF, KEY = (PIECES < 16 ? PIECES : 16) - 1;        // 16-byte pieces of a row; piece c of row r lies at c ^ (r & KEY)
@@ -138,14 +139,15 @@ __device__ __forceinline__ void mx_store_sums(float* sums, int splits, unsigned 
     }
 }
 
-template <int FMT, int RF, int CF>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RF * CF > 8 ? 1 : 2)))
+template <int FMT, int RF, int CF, int SLOTS>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MxTileShape<FMT, RF, CF, SLOTS>::WAVES)))
 gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __restrict__ partial, int* __restrict__ arrived, GemmEpilogue ep) {
-    using T = MxTileShape<FMT, RF, CF>;
+    using T = MxTileShape<FMT, RF, CF, SLOTS>;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
     const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<size_t>((__attribute__((address_space(3))) void*)(lds_raw)));
     const int n_tiles = (p.n + T::COLS - 1) / T::COLS;
-    const int m_tiles = mx_row_tiles<T::ROWS>(p);
+    const MxTiles<T::ROWS> row_tiles(p);
+    const int m_tiles = row_tiles.total;
     const int units = m_tiles * n_tiles * splits, per_xcd = (units + 7) >> 3;
     const int local = static_cast<int>(blockIdx.x >> 3), unit = static_cast<int>(blockIdx.x & 7) * per_xcd + local;     // each XCD a contiguous range (see pp_unit)
     if (local >= per_xcd || unit >= units) return;
@@ -158,7 +160,7 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
         n_tile = rest / splits;
         split = rest - n_tile * splits;
     }
-    const MxTile t = mx_find_tile<T::ROWS>(p, m_tile);
+    const MxTile t = row_tiles.find(p, m_tile);
     const int n0 = n_tile * T::COLS, n32 = (p.n + 31) & ~31;
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -246,11 +248,12 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
         }
     };
     typedef std::integral_constant<int, 0> zero;
+    constexpr int FIRST = T::COPIES / 2;
     copies(0, 0, zero{}, std::integral_constant<int, T::COPIES + SC>{}, copies);
     copies(1, T::SLOT, zero{}, std::integral_constant<int, T::COPIES>{}, copies);
-    copies(2, 2 * T::SLOT, zero{}, std::integral_constant<int, T::COPIES + SC>{}, copies);
-    copies(3, 3 * T::SLOT, zero{}, std::integral_constant<int, T::COPIES / 2>{}, copies);
-    pp_wait<2 * T::COPIES + SC + T::COPIES / 2>();
+    if constexpr (SLOTS == 4) copies(2, 2 * T::SLOT, zero{}, std::integral_constant<int, T::COPIES + SC>{}, copies);
+    copies(SLOTS - 1, (SLOTS - 1) * T::SLOT, zero{}, std::integral_constant<int, FIRST>{}, copies);
+    pp_wait<(SLOTS == 4 ? 2 * T::COPIES + SC : T::COPIES) + FIRST>();
     pp_barrier();
 
     u32x4 af[2][RF], wf[2][CF];
@@ -278,19 +281,18 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
     typedef std::integral_constant<int, RF + CF> operands;
     each(zero{}, operands{}, [&](auto f) { read(0, zero{}, zero{}, f); read_scale(0, zero{}, f); }, each);
 
-    // Phase P (0..3) of step `s`, whose half steps lie in slot `lo` and the one behind it: its instructions, between them the reads of the next phase and the copies of the half step four on.
-    // Copies into the slot of half step h start in its second phase, behind the barrier that all waves reach with their reads of it done, and end in the phase after that.
-    auto phase = [&](int s, unsigned lo, auto pc) __attribute__((always_inline)) {
-        constexpr int P = decltype(pc)::value, B = P & 1;        // operands are in buffer B
-        const unsigned hi = lo + T::SLOT, next = 2 * T::SLOT - lo;
-        constexpr int COUNT = RF * CF, FIRST = T::COPIES / 2;
-        // copies of this phase: second phase of a half step: the first share of the half step four on; first phase: the rest of the one three on
-        constexpr bool EVEN = P == 1 || P == 2;                                           // the half step that is copied is an even one, with scales
-        constexpr int C0 = (P & 1) ? 0 : FIRST, C1 = (P & 1) ? FIRST : T::COPIES + (EVEN ? SC : 0);
-        const int ch = P == 0 ? 2 * s + 3 : P == 1 ? 2 * s + 4 : P == 2 ? 2 * s + 4 : 2 * s + 5;
-        const unsigned cslot = P == 0 ? next + T::SLOT : P == 1 || P == 2 ? lo : hi;
+    // Phase P (0..3) of step `s`, whose half steps lie in slots `lo` and `hi`: its instructions, between them the reads of the next phase and copies.  Copies into the slot of a half step
+    // start in its second phase, behind the barrier that all waves reach with their reads of it done, and end in the phase after that; a half step's copies have landed when those
+    // of the SLOTS - 2 half steps after it are in flight.
+    auto phase = [&](int s, unsigned lo, unsigned hi, auto pc) __attribute__((always_inline)) {
+        constexpr int P = decltype(pc)::value, B = P & 1, COUNT = RF * CF;                // operands are in buffer B
+        constexpr int AHEAD = P == 0 ? SLOTS - 1 : P == 3 ? SLOTS + 1 : SLOTS;            // half step 2 s + AHEAD is copied: its first share in odd phases, the rest in even ones
+        constexpr int C0 = (P & 1) ? 0 : FIRST, C1 = (P & 1) ? FIRST : T::COPIES + (AHEAD % 2 == 0 ? SC : 0);
+        const int ch = 2 * s + AHEAD;
+        const unsigned cslot = P == 0 ? (lo == 0 ? (SLOTS - 1) * T::SLOT : lo - T::SLOT) : P == 3 ? hi : lo;
+        const unsigned next = hi == (SLOTS - 1) * T::SLOT ? 0 : hi + T::SLOT;
         if constexpr (P & 1) {
-            pp_wait<2 * T::COPIES + SC>();
+            pp_wait<SLOTS == 4 ? 2 * T::COPIES + SC : T::COPIES + (P == 1 ? SC : 0)>();
             pp_barrier();
         }
         each(zero{}, std::integral_constant<int, COUNT>{}, [&](auto qc) __attribute__((always_inline)) {
@@ -311,12 +313,14 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
     };
     typedef std::integral_constant<int, 2> two;
     typedef std::integral_constant<int, 3> three;
+    unsigned lo = 0;
     for (int s = 0; s < n_steps; ++s) {
-        const unsigned lo = (s & 1) ? 2 * T::SLOT : 0u;
-        phase(s, lo, zero{});
-        phase(s, lo, one{});
-        phase(s, lo, two{});
-        phase(s, lo, three{});
+        const unsigned hi = lo == (SLOTS - 1) * T::SLOT ? 0 : lo + T::SLOT;
+        phase(s, lo, hi, zero{});
+        phase(s, lo, hi, one{});
+        phase(s, lo, hi, two{});
+        phase(s, lo, hi, three{});
+        lo = hi == (SLOTS - 1) * T::SLOT ? 0 : hi + T::SLOT;
 #pragma unroll
         for (int j = 0; j < CF; ++j) ws[0][j] = ws[1][j];
 #pragma unroll
@@ -357,9 +361,9 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
     else mx_store<RF, CF, T::STORE_ROWS, false>(acc, own, t, p.n, m0, n0w, ep);
 }
 
-template <int FMT, int RF, int CF>
+template <int FMT, int RF, int CF, int SLOTS>
 int launch_mx_tile(regione_ctx* ctx, const MxOperands& p, int splits, const GemmEpilogue& ep) {
-    using T = MxTileShape<FMT, RF, CF>;
+    using T = MxTileShape<FMT, RF, CF, SLOTS>;
     static std::atomic<uint64_t> granted{0};
     const int64_t row_tiles = mx_most_row_tiles(p, T::ROWS), n_tiles = (p.n + T::COLS - 1) / T::COLS;
     const int per = (p.steps + splits - 1) / splits, used = (p.steps + per - 1) / per;
@@ -367,8 +371,8 @@ int launch_mx_tile(regione_ctx* ctx, const MxOperands& p, int splits, const Gemm
         RG_FAIL(REGIONE_ERR_WORKSPACE, "linear: %d K-splits of a %d x %d result exceed the workspace", used, p.m, p.n);
     const int64_t workgroups = (row_tiles * n_tiles * used + 7) / 8 * 8;
     if (workgroups >= (int64_t{1} << 32) / T::THREADS) RG_FAIL(REGIONE_ERR_UNSUPPORTED, "linear: a result of %d x %d", p.m, p.n);
-    if (int rc = rg_grant_lds(ctx, reinterpret_cast<const void*>(gemm_mx_tile_kernel<FMT, RF, CF>), granted, T::LDS_BYTES)) return rc;
-    hipLaunchKernelGGL((gemm_mx_tile_kernel<FMT, RF, CF>), dim3(static_cast<unsigned>(workgroups)), dim3(T::THREADS), T::LDS_BYTES, ctx->stream, p, used, per, ctx->gemm_part, ctx->gemm_arrived, ep);
+    if (int rc = rg_grant_lds(ctx, reinterpret_cast<const void*>(gemm_mx_tile_kernel<FMT, RF, CF, SLOTS>), granted, T::LDS_BYTES)) return rc;
+    hipLaunchKernelGGL((gemm_mx_tile_kernel<FMT, RF, CF, SLOTS>), dim3(static_cast<unsigned>(workgroups)), dim3(T::THREADS), T::LDS_BYTES, ctx->stream, p, used, per, ctx->gemm_part, ctx->gemm_arrived, ep);
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }
@@ -376,14 +380,17 @@ int launch_mx_tile(regione_ctx* ctx, const MxOperands& p, int splits, const Gemm
 template <int FMT>
 int launch_mx_tile(regione_ctx* ctx, int tile, const MxOperands& p, int splits, const GemmEpilogue& ep) {
     switch (tile) {
-        case 44: return launch_mx_tile<FMT, 4, 4>(ctx, p, splits, ep);
-        case 34: return launch_mx_tile<FMT, 3, 4>(ctx, p, splits, ep);
-        case 24: return launch_mx_tile<FMT, 2, 4>(ctx, p, splits, ep);
-        case 42: return launch_mx_tile<FMT, 4, 2>(ctx, p, splits, ep);
-        case 22: return launch_mx_tile<FMT, 2, 2>(ctx, p, splits, ep);
-        case 12: return launch_mx_tile<FMT, 1, 2>(ctx, p, splits, ep);
-        case 21: return launch_mx_tile<FMT, 2, 1>(ctx, p, splits, ep);
-        case 11: return launch_mx_tile<FMT, 1, 1>(ctx, p, splits, ep);
+        case 44: return launch_mx_tile<FMT, 4, 4, 4>(ctx, p, splits, ep);
+        case 324: return launch_mx_tile<FMT, 2, 4, 3>(ctx, p, splits, ep);
+        case 342: return launch_mx_tile<FMT, 4, 2, 3>(ctx, p, splits, ep);
+        case 322: return launch_mx_tile<FMT, 2, 2, 3>(ctx, p, splits, ep);
+        case 34: return launch_mx_tile<FMT, 3, 4, 4>(ctx, p, splits, ep);
+        case 24: return launch_mx_tile<FMT, 2, 4, 4>(ctx, p, splits, ep);
+        case 42: return launch_mx_tile<FMT, 4, 2, 4>(ctx, p, splits, ep);
+        case 22: return launch_mx_tile<FMT, 2, 2, 4>(ctx, p, splits, ep);
+        case 12: return launch_mx_tile<FMT, 1, 2, 4>(ctx, p, splits, ep);
+        case 21: return launch_mx_tile<FMT, 2, 1, 4>(ctx, p, splits, ep);
+        case 11: return launch_mx_tile<FMT, 1, 1, 4>(ctx, p, splits, ep);
     }
     RG_FAIL(REGIONE_ERR_INVALID_ARG, "linear: no tile %d", tile);
 }

@@ -80,37 +80,40 @@ __device__ __forceinline__ int64_t scale_at(int layout, int64_t row, int block, 
     return layout == REGIONE_MX_SCALE_STEPS ? mx_scale_step(row, block, padded_rows) : row * blocks + block;
 }
 
-// A unit is the part of a row inside one step of 256 values: half a wave, eight values per lane, four lanes per block.
+// Half a wave takes the part of a row inside one step of 256 values: eight values per lane, four lanes per block.  A workgroup's eight halves take U such parts each, of
+// 16 rows (eight, U = 1) and the U / 2 steps beside each other, so that the line of memory that holds a step's scales of 16 rows is written by one workgroup.
 // HBM bound: 2 or 4 bytes in and 0.53 out per value.
-template <typename T>
+template <typename T, int U>
 __global__ void __launch_bounds__(kThreads)
 quantize_rows_mxfp4_kernel(const T* __restrict__ x, int64_t rows, int cols, int layout, uint8_t* __restrict__ q, uint8_t* __restrict__ scale) {
-    const int steps = (cols + kMxStep - 1) / kMxStep, blocks = cols / kMxBlock;
-    const int64_t units = rows * steps, stride = static_cast<int64_t>(gridDim.x) * (kThreads / 32), padded = mx_padded_rows(rows);
-    const int l32 = threadIdx.x & 31;
-    int64_t unit = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
-    for (; unit < units; unit += stride * kUnroll) {
-        Eight<T> v[kUnroll];
-        int64_t row[kUnroll];
-        int col[kUnroll];
+    constexpr int R = U == 1 ? 8 : 16, S = 8 * U / R;                  // rows and steps of a workgroup
+    const int steps = (cols + kMxStep - 1) / kMxStep, blocks = cols / kMxBlock, across = (steps + S - 1) / S;
+    const int64_t padded = mx_padded_rows(rows);
+    const int l32 = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const int64_t panels = (rows + R - 1) / R * across;
+    for (int64_t at = blockIdx.x; at < panels; at += gridDim.x) {      // (once but for calls of 2^20 panels and more)
+        const int64_t panel = at / across;
+        const int step0 = static_cast<int>(at - panel * across) * S;
+        Eight<T> v[U];
 #pragma unroll
-        for (int i = 0; i < kUnroll; ++i) {
-            const int64_t u = unit + i * stride;
-            row[i] = u / steps;
-            col[i] = static_cast<int>(u - row[i] * steps) * kMxStep + 8 * l32;
-            if (u < units && col[i] < cols) v[i].load(x + row[i] * cols + col[i]);
+        for (int i = 0; i < U; ++i) {
+            const int64_t row = panel * R + (8 * i + part) % R;
+            const int col = (step0 + (8 * i + part) / R) * kMxStep + 8 * l32;
+            if (row < rows && col < cols) v[i].load(x + row * cols + col);
             else v[i].clear();
         }
 #pragma unroll
-        for (int i = 0; i < kUnroll; ++i) {
-            if (unit + i * stride >= units) continue;
+        for (int i = 0; i < U; ++i) {
+            const int64_t row = panel * R + (8 * i + part) % R;
+            const int step = step0 + (8 * i + part) / R, col = step * kMxStep + 8 * l32;
+            if (row >= rows || step >= steps) continue;
             const unsigned top = block_max(v[i].top());
             const unsigned byte = top == 255u ? 255u : top > 2u ? top - 2u : 0u;
             const unsigned codes = top == 255u ? 0u : v[i].codes(mx_scale_value(byte));
-            if (col[i] < cols) *reinterpret_cast<unsigned*>(q + (row[i] * cols + col[i]) / 2) = codes;
-            const int block = col[i] / kMxBlock;
+            if (col < cols) *reinterpret_cast<unsigned*>(q + (row * cols + col) / 2) = codes;
+            const int block = col / kMxBlock;
             if ((l32 & 3) == 0 && (block < blocks || layout == REGIONE_MX_SCALE_STEPS))    // (a step's blocks past the row's end are zero)
-                scale[scale_at(layout, row[i], block, blocks, padded)] = static_cast<uint8_t>(byte);
+                scale[scale_at(layout, row, block, blocks, padded)] = static_cast<uint8_t>(byte);
         }
     }
 }
@@ -192,6 +195,11 @@ unsigned row_workgroups(int64_t rows, int cols) {
     return static_cast<unsigned>(want < (1 << 20) ? want : 1 << 20);
 }
 
+template <typename T, int U>
+void launch_quantize(regione_ctx* ctx, dim3 grid, const void* x, int64_t rows, int cols, int layout, void* q, void* scale) {
+    hipLaunchKernelGGL((quantize_rows_mxfp4_kernel<T, U>), grid, dim3(kThreads), 0, ctx->stream, static_cast<const T*>(x), rows, cols, layout, static_cast<uint8_t*>(q), static_cast<uint8_t*>(scale));
+}
+
 int check_rows(regione_ctx* ctx, const char* who, int64_t rows, int32_t cols, int32_t layout) {
     if (!ctx) RG_FAIL(REGIONE_ERR_INVALID_ARG, "%s: null context", who);
     if (layout != REGIONE_MX_SCALE_ROWS && layout != REGIONE_MX_SCALE_STEPS) RG_FAIL(REGIONE_ERR_INVALID_ARG, "%s: scale layout %d", who, layout);
@@ -208,9 +216,17 @@ extern "C" int regione_quantize_rows_mxfp4(regione_ctx* ctx, const void* x, int3
     if (rows == 0) return REGIONE_OK;
     if (!x || !q || !scale || !rg_aligned16(x) || !rg_aligned16(q) || !rg_aligned16(scale)) RG_FAIL(REGIONE_ERR_INVALID_ARG, "quantize_rows_mxfp4: null or unaligned tensor");
     ProfScope prof(ctx, REGIONE_PROF_ROWS);
-    const dim3 grid(row_workgroups(rows, cols));
-    if (x_dtype == REGIONE_FP32) hipLaunchKernelGGL(quantize_rows_mxfp4_kernel<float>, grid, dim3(kThreads), 0, ctx->stream, static_cast<const float*>(x), rows, cols, scale_layout, static_cast<uint8_t*>(q), static_cast<uint8_t*>(scale));
-    else hipLaunchKernelGGL(quantize_rows_mxfp4_kernel<bf16_t>, grid, dim3(kThreads), 0, ctx->stream, static_cast<const bf16_t*>(x), rows, cols, scale_layout, static_cast<uint8_t*>(q), static_cast<uint8_t*>(scale));
+    const int64_t steps = (cols + kMxStep - 1) / kMxStep;
+    if (rows * steps < 8192) {                                 // fewer than 1024 workgroups: one part each
+        const dim3 grid(static_cast<unsigned>((rows + 7) / 8 * steps));
+        if (x_dtype == REGIONE_FP32) launch_quantize<float, 1>(ctx, grid, x, rows, cols, scale_layout, q, scale);
+        else launch_quantize<bf16_t, 1>(ctx, grid, x, rows, cols, scale_layout, q, scale);
+    } else {
+        const int64_t workgroups = (rows + 15) / 16 * ((steps + 1) / 2);
+        const dim3 grid(static_cast<unsigned>(workgroups < (1 << 20) ? workgroups : 1 << 20));
+        if (x_dtype == REGIONE_FP32) launch_quantize<float, 4>(ctx, grid, x, rows, cols, scale_layout, q, scale);
+        else launch_quantize<bf16_t, 4>(ctx, grid, x, rows, cols, scale_layout, q, scale);
+    }
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }
