@@ -12,28 +12,30 @@
 
 namespace {
 
-// Copy of 16 bytes per lane into LDS (see pp_copy16) by the lanes of `lanes`; a copy that nobody wants keeps its place in the wave's count.
-__device__ __forceinline__ void mx_copy16(unsigned lane_off, const void* base, unsigned lds_base, uint64_t lanes) {
-    asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1"
-                 :: "v"(lane_off), "s"(base), "s"(lds_base), "s"(lanes) : "memory", "m0");
+// One or two copies of 16 bytes per lane into LDS, the second one's 1 KiB behind the first (its lane offset is 1 KiB less than its address): the counterpart of pp_copy16 through a
+// buffer resource, whose size makes accesses past the end of a tensor, and all of a half step that does not exist, into reads of nothing.
+__device__ __forceinline__ void mx_copy(unsigned lane_off, const u32x4& rsrc, unsigned lds_base) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" :: "v"(lane_off), "s"(rsrc), "s"(lds_base) : "memory", "m0");
 }
-
-// all lanes where a < b, none elsewhere (in scalar registers, which the compiler's own selection of such a mask leaves)
-__device__ __forceinline__ uint64_t mx_lanes_if(int a, int b) {
-    uint64_t lanes;
-    asm("s_cmp_lt_i32 %1, %2\n\ts_cselect_b64 %0, -1, 0" : "=s"(lanes) : "s"(a), "s"(b) : "scc");
-    return lanes;
+__device__ __forceinline__ void mx_copy(unsigned lane_off, unsigned lane_off2, const u32x4& rsrc, unsigned lds_base) {
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds\n\tbuffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds"
+                 :: "v"(lane_off), "v"(lane_off2), "s"(rsrc), "s"(lds_base) : "memory", "m0");
 }
+// A source of copies: `at` moves on by a stride per (half) step, `left` are the bytes from there to the end of what may be read.
+struct MxSource {
+    uint64_t at; int left;
+    __device__ __forceinline__ u32x4 rsrc(bool there) const { return u32x4{static_cast<unsigned>(at), static_cast<unsigned>(at >> 32), there ? static_cast<unsigned>(left) : 0u, 0x00027000u}; }
+};
 
 template <int FMT, int RF, int CF, int SLOTS> struct MxTileShape {
     static constexpr int ROWS = 64 * RF, COLS = 64 * CF, THREADS = 256;
     static constexpr int COPIES = RF + CF;                          // 1 KiB copies per wave and half step: RF of 16 rows, CF of a weight block's 64 inputs
     static constexpr unsigned SLOT = (ROWS + COLS) * 64u, W_BASE = ROWS * 64u;
-    static constexpr unsigned SCALES = FMT == MX_FP4 ? (ROWS + COLS) * 8u : 0u, S_BASE = SLOTS * SLOT;      // of a whole step; two of them
+    static constexpr unsigned SCALES = FMT == MX_FP4 ? 4096u : 0u, S_BASE = SLOTS * SLOT;       // of a whole step, 1 KiB per wave: rows 0.., 128.., columns 0.., 128..; two of them
     static constexpr unsigned LDS_BYTES = S_BASE + 2 * SCALES;
     static constexpr int STORE_ROWS = RF % 2 == 0 && 2 * CF * 16384u <= LDS_BYTES ? 2 : 1;                   // rows of fragments per wave that mx_store leaves in LDS at a time
     static_assert(STORE_ROWS * CF * 16384u <= LDS_BYTES, "four waves' fragments");
-    static constexpr int FIT = 163840 / LDS_BYTES, WAVES = RF * CF > 8 ? 1 : FIT < 2 ? 2 : FIT > 4 ? 4 : FIT;    // workgroups that a CU's LDS holds; waves per SIMD that registers are kept for
+    static constexpr int FIT = 163840 / LDS_BYTES, WAVES = RF * CF > 8 ? 1 : RF * CF > 2 ? 2 : FIT > 4 ? 4 : FIT;    // workgroups that a CU's LDS holds; waves per SIMD that registers are kept for
     static constexpr int64_t PART_FLOATS = static_cast<int64_t>(ROWS) * COLS;
 };
 
@@ -160,6 +162,8 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
         n_tile = rest / splits;
         split = rest - n_tile * splits;
     }
+    // (the divisions leave these in vector registers, and everything that follows from them)
+    m_tile = __builtin_amdgcn_readfirstlane(m_tile); n_tile = __builtin_amdgcn_readfirstlane(n_tile); split = __builtin_amdgcn_readfirstlane(split);
     const MxTile t = row_tiles.find(p, m_tile);
     const int n0 = n_tile * T::COLS, n32 = (p.n + 31) & ~31;
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
@@ -170,44 +174,37 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
     n_steps = n_steps < steps_per_split ? n_steps : steps_per_split;
     const int n_half = 2 * n_steps;
 
-    // Copy sources.  A: a lane copies 16 bytes of a row's 64; chunk c of row r lies at c ^ ((r >> 2) & 3), so that sixteen rows' same chunk covers all banks once.
+    // Copy sources.  A: a lane copies 16 bytes of a row's 64; chunk c of row r lies at c ^ ((r >> 2) & 3), so that sixteen rows' same chunk covers all banks once.  Rows past the tensor's
+    // end read nothing; past a row's end the next row's values are read, which meet weights of zero (bf16 rows are whole steps), and E2M1 has neither NaN nor infinity.
     unsigned a_voff[RF];
 #pragma unroll
-    for (int i = 0; i < RF; ++i) {
-        int r = (wave * RF + i) * 16 + (lane >> 2);
-        r = t.row0 + r < t.end ? r : t.end - 1 - t.row0;                           // rows past the end repeat the last one; their results are not stored
-        a_voff[i] = static_cast<unsigned>(r) * static_cast<unsigned>(p.row_bytes) + static_cast<unsigned>((lane & 3) ^ ((lane >> 4) & 3)) * 16u;
-    }
-    const int a_live = (t.end - t.row0 - wave * (RF * 16) + 15) >> 4;              // nor are they copied where a whole copy is
-    const uint8_t* a_base = p.a + static_cast<int64_t>(t.row0) * p.row_bytes + static_cast<int64_t>(step0) * 128;
-    const int a_left = p.row_bytes - step0 * 128;                                  // bytes of a row from here on; past them the weights are zero, and what LDS holds will do
-    const int a_chunk = ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+    for (int i = 0; i < RF; ++i)
+        a_voff[i] = static_cast<unsigned>((wave * RF + i) * 16 + (lane >> 2)) * static_cast<unsigned>(p.row_bytes) + static_cast<unsigned>((lane & 3) ^ ((lane >> 4) & 3)) * 16u + (i % 2 == 1 ? 0u : 1024u);
+    const int64_t a_first = static_cast<int64_t>(t.row0) * p.row_bytes + static_cast<int64_t>(step0) * 128 - 1024;     // (the second copy of a pair adds 1 KiB by itself)
+    const int64_t a_left = static_cast<int64_t>(p.m) * p.row_bytes - a_first;
+    MxSource a = {reinterpret_cast<uint64_t>(p.a) + a_first, static_cast<int>(a_left < INT32_MAX ? a_left : INT32_MAX)};
     // W: a block's 64 inputs are one fragment; its 32 features are put in the order that leaves a lane with twice eight consecutive results beside those of the row's other lane:
     // place 8*g + 4*h + u, whose results lane half h holds in registers 4*g + u, gets feature 16*(g/2) + 8*h + 4*(g%2) + u.
-    const uint8_t* w = p.w + t.weight * p.w_stride;
-    const unsigned feature = (l32 >> 4) * 16 + ((l32 >> 2) & 1) * 8 + ((l32 >> 3) & 1) * 4 + (l32 & 3), w_voff = ((lane & 32) + feature) * 16u;
-    const uint8_t* w_base[CF];
+    const uint8_t* w_all = p.w + t.weight * p.w_stride;
+    const unsigned feature = (l32 >> 4) * 16 + ((l32 >> 2) & 1) * 8 + ((l32 >> 3) & 1) * 4 + (l32 & 3);
+    unsigned w_voff[CF];
 #pragma unroll
     for (int j = 0; j < CF; ++j) {
         const int piece = wave * CF + j;                                           // piece / 2: block of the tile, piece % 2: phase of the half step
-        int nb = (n0 >> 5) + (piece >> 1);
-        nb = nb < n32 / 32 ? nb : n32 / 32 - 1;                                    // blocks past N repeat the last one
-        w_base[j] = w + ((static_cast<int64_t>(nb) * p.steps + step0) * 4 + (piece & 1)) * 1024;
+        int nb = piece >> 1;
+        nb = (n0 >> 5) + nb < n32 / 32 ? nb : n32 / 32 - 1 - (n0 >> 5);            // blocks past N repeat the last one
+        w_voff[j] = static_cast<unsigned>(nb) * static_cast<unsigned>(p.steps) * 4096u + (piece & 1) * 1024u + ((lane & 32) + feature) * 16u + (j % 2 == 1 ? 0u : 1024u);
     }
+    MxSource w = {reinterpret_cast<uint64_t>(w_all) + (static_cast<int64_t>(n0 >> 5) * p.steps + step0) * 4096 - 1024, INT32_MAX};
     // scales of a step: waves 0 and 1 copy those of the rows, waves 2 and 3 of the columns, 16 bytes (two rows) per lane
-    const uint8_t* s_base = nullptr;
-    unsigned s_voff = 0, s_dst = 0;
+    MxSource scales = {0, INT32_MAX};
+    unsigned s_voff = 0;
     int64_t s_step = 0;
-    uint64_t s_lanes = 0;
     if (FMT == MX_FP4) {
-        const int pair = (wave & 1) * 64 + lane;
-        const int count = wave < 2 ? T::ROWS / 2 : T::COLS / 2, first = wave < 2 ? t.row0 / 2 : n0 / 2;
-        const int last = (wave < 2 ? static_cast<int>(mx_padded_rows(p.m)) : n32) / 2 - 1;
-        s_lanes = __ballot(pair < count);
-        s_voff = static_cast<unsigned>((first + pair < last ? first + pair : last) - first) * 16u;
+        const int first = wave < 2 ? t.row0 / 2 : n0 / 2, last = (wave < 2 ? static_cast<int>(mx_padded_rows(p.m)) : n32) / 2 - 1 - first, pair = (wave & 1) * 64 + lane;
+        s_voff = static_cast<unsigned>(pair < last ? pair : last) * 16u;           // pairs past the end repeat the last one
         s_step = (wave < 2 ? mx_padded_rows(p.m) : n32) * 8;
-        s_base = (wave < 2 ? p.a_scale : w + static_cast<int64_t>(n32) * p.steps * 128) + step0 * s_step + static_cast<int64_t>(first) * 16;
-        s_dst = lds0 + T::S_BASE + (wave < 2 ? 0u : T::ROWS * 8u) + (wave & 1) * 1024u;
+        scales.at = reinterpret_cast<uint64_t>(wave < 2 ? p.a_scale : w_all + static_cast<int64_t>(n32) * p.steps * 128) + step0 * s_step + static_cast<int64_t>(first) * 16;
     }
 
     // LDS addresses of the fragments
@@ -216,7 +213,7 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
     for (int q = 0; q < 2; ++q) a_off[q] = static_cast<unsigned>(wm * (RF * 32) + l32) * 64u + static_cast<unsigned>(((2 * q + half) ^ ((l32 >> 2) & 3)) << 4);
     const unsigned w_off = T::W_BASE + static_cast<unsigned>(wn * CF) * 2048u + lane * 16u;
     const unsigned as_off = T::S_BASE + static_cast<unsigned>(wm * (RF * 32) + l32) * 8u + half * 4u;
-    const unsigned ws_off = T::S_BASE + T::ROWS * 8u + (static_cast<unsigned>(wn * (CF * 32)) + feature) * 8u + half * 4u;
+    const unsigned ws_off = T::S_BASE + 2048u + (static_cast<unsigned>(wn * (CF * 32)) + feature) * 8u + half * 4u;
 
     f32x16 acc[RF][CF];
 #pragma unroll
@@ -226,34 +223,42 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    // Copy number C of half step H into its slot: 0..RF-1 rows, RF.. weights, and for even half steps one of scales at the end.
-    auto copy = [&](int h, unsigned slot, auto index) __attribute__((always_inline)) {
-        constexpr int C = decltype(index)::value;
-        // (no branches: the accumulators' instructions would be moved across them)
-        const uint64_t there = mx_lanes_if(h, n_half);
-        if constexpr (C < RF) {
-            const uint64_t row_lanes = __ballot(a_chunk < a_left - h * 64);
-            mx_copy16(a_voff[C], a_base + static_cast<int64_t>(h) * 64, lds0 + slot + (wave * RF + C) * 1024u, there & mx_lanes_if(C, a_live) & row_lanes);
-        } else if constexpr (C < RF + CF) {
-            mx_copy16(w_voff, w_base[C - RF] + static_cast<int64_t>(h) * 2048, lds0 + slot + T::W_BASE + (wave * CF + (C - RF)) * 1024u, there);
+    // Copies come in pairs; sources move on with the last one of a half step.  (No branches: the accumulators' instructions would be moved across them.)
+    auto copy_pair = [&](MxSource& from, const auto& voff, bool there, unsigned to, auto index, int stride) __attribute__((always_inline)) {
+        constexpr int C = 2 * decltype(index)::value, N = sizeof(voff) / sizeof(voff[0]);
+        if constexpr (C + 1 < N) mx_copy(voff[C], voff[C + 1], from.rsrc(there), to + C * 1024u);
+        else mx_copy(voff[C], from.rsrc(there), to + C * 1024u);
+        if constexpr (C + 2 >= N) from.at += static_cast<int64_t>(stride);
+    };
+    constexpr int A_PAIRS = (RF + 1) / 2, W_PAIRS = (CF + 1) / 2;
+    constexpr int SC = FMT == MX_FP4 ? 1 : 0;
+    // number C of the copies of half step h into its slot: rows; weights, and for even half steps scales behind them
+    auto copy_a = [&](int h, unsigned slot, auto c) __attribute__((always_inline)) {
+        copy_pair(a, a_voff, h < n_half, lds0 + slot + wave * (RF * 1024u), c, 64);
+        if constexpr (decltype(c)::value == A_PAIRS - 1) asm("s_sub_i32 %0, %0, 64\n\ts_max_i32 %0, %0, 0" : "+s"(a.left) : : "scc");     // (left to itself the compiler subtracts in a vector register)
+    };
+    auto copy_w = [&](int h, unsigned slot, auto c) __attribute__((always_inline)) {
+        if constexpr (decltype(c)::value < W_PAIRS) {
+            copy_pair(w, w_voff, h < n_half, lds0 + slot + T::W_BASE + wave * (CF * 1024u), c, 2048);
         } else {
-            mx_copy16(s_voff, s_base + (h >> 1) * s_step, s_dst + ((h >> 1) & 1) * T::SCALES, there & s_lanes);
+            mx_copy(s_voff, scales.rsrc(h < n_half), lds0 + T::S_BASE + ((h >> 1) & 1) * T::SCALES + wave * 1024u);
+            scales.at += s_step;
         }
     };
-    constexpr int SC = FMT == MX_FP4 ? 1 : 0;
-    auto copies = [&](int h, unsigned slot, auto from, auto to, auto self) __attribute__((always_inline)) {
+    auto each = [&](auto from, auto to, auto f, auto self) __attribute__((always_inline)) {
         if constexpr (decltype(from)::value < decltype(to)::value) {
-            copy(h, slot, from);
-            self(h, slot, std::integral_constant<int, decltype(from)::value + 1>{}, to, self);
+            f(from);
+            self(std::integral_constant<int, decltype(from)::value + 1>{}, to, f, self);
         }
     };
     typedef std::integral_constant<int, 0> zero;
-    constexpr int FIRST = T::COPIES / 2;
-    copies(0, 0, zero{}, std::integral_constant<int, T::COPIES + SC>{}, copies);
-    copies(1, T::SLOT, zero{}, std::integral_constant<int, T::COPIES>{}, copies);
-    if constexpr (SLOTS == 4) copies(2, 2 * T::SLOT, zero{}, std::integral_constant<int, T::COPIES + SC>{}, copies);
-    copies(SLOTS - 1, (SLOTS - 1) * T::SLOT, zero{}, std::integral_constant<int, FIRST>{}, copies);
-    pp_wait<(SLOTS == 4 ? 2 * T::COPIES + SC : T::COPIES) + FIRST>();
+    typedef std::integral_constant<int, A_PAIRS> a_pairs;
+    each(zero{}, std::integral_constant<int, SLOTS>{}, [&](auto hc) __attribute__((always_inline)) {
+        constexpr int H = decltype(hc)::value;
+        each(zero{}, a_pairs{}, [&](auto c) __attribute__((always_inline)) { copy_a(H, H * T::SLOT, c); }, each);
+        if constexpr (H < SLOTS - 1) each(zero{}, std::integral_constant<int, W_PAIRS + (H % 2 == 0 ? SC : 0)>{}, [&](auto c) __attribute__((always_inline)) { copy_w(H, H * T::SLOT, c); }, each);
+    }, each);
+    pp_wait<(SLOTS == 4 ? 2 * T::COPIES + SC : T::COPIES) + RF>();
     pp_barrier();
 
     u32x4 af[2][RF], wf[2][CF];
@@ -271,12 +276,6 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
             else as[B][F - CF] = *reinterpret_cast<const unsigned*>(lds_raw + (as_off + which) + (F - CF) * 256);
         }
     };
-    auto each = [&](auto from, auto to, auto f, auto self) __attribute__((always_inline)) {
-        if constexpr (decltype(from)::value < decltype(to)::value) {
-            f(from);
-            self(std::integral_constant<int, decltype(from)::value + 1>{}, to, f, self);
-        }
-    };
     typedef std::integral_constant<int, 1> one;
     typedef std::integral_constant<int, RF + CF> operands;
     each(zero{}, operands{}, [&](auto f) { read(0, zero{}, zero{}, f); read_scale(0, zero{}, f); }, each);
@@ -286,8 +285,8 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
     // of the SLOTS - 2 half steps after it are in flight.
     auto phase = [&](int s, unsigned lo, unsigned hi, auto pc) __attribute__((always_inline)) {
         constexpr int P = decltype(pc)::value, B = P & 1, COUNT = RF * CF;                // operands are in buffer B
-        constexpr int AHEAD = P == 0 ? SLOTS - 1 : P == 3 ? SLOTS + 1 : SLOTS;            // half step 2 s + AHEAD is copied: its first share in odd phases, the rest in even ones
-        constexpr int C0 = (P & 1) ? 0 : FIRST, C1 = (P & 1) ? FIRST : T::COPIES + (AHEAD % 2 == 0 ? SC : 0);
+        constexpr int AHEAD = P == 0 ? SLOTS - 1 : P == 3 ? SLOTS + 1 : SLOTS;            // of half step 2 s + AHEAD the rows are copied in odd phases, the weights and scales in even ones
+        constexpr int PAIRS = (P & 1) ? A_PAIRS : W_PAIRS + (AHEAD % 2 == 0 ? SC : 0);
         const int ch = 2 * s + AHEAD;
         const unsigned cslot = P == 0 ? (lo == 0 ? (SLOTS - 1) * T::SLOT : lo - T::SLOT) : P == 3 ? hi : lo;
         const unsigned next = hi == (SLOTS - 1) * T::SLOT ? 0 : hi + T::SLOT;
@@ -306,8 +305,10 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
                 else if constexpr (P == 2) read(hi, one{}, one{}, f);
                 else { read(next, zero{}, zero{}, f); read_scale(((s + 1) & 1) * T::SCALES, one{}, f); }
             }, each);
-            constexpr int N = C1 - C0, K0 = C0 + Q * N / COUNT, K1 = C0 + (Q + 1) * N / COUNT;
-            copies(ch, cslot, std::integral_constant<int, K0>{}, std::integral_constant<int, K1>{}, copies);
+            each(std::integral_constant<int, Q * PAIRS / COUNT>{}, std::integral_constant<int, (Q + 1) * PAIRS / COUNT>{}, [&](auto c) __attribute__((always_inline)) {
+                if constexpr (P & 1) copy_a(ch, cslot, c);
+                else copy_w(ch, cslot, c);
+            }, each);
             __builtin_amdgcn_sched_barrier(0);
         }, each);
     };
