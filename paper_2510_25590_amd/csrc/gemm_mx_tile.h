@@ -27,15 +27,16 @@ struct MxSource {
     __device__ __forceinline__ u32x4 rsrc(bool there) const { return u32x4{static_cast<unsigned>(at), static_cast<unsigned>(at >> 32), there ? static_cast<unsigned>(left) : 0u, 0x00027000u}; }
 };
 
-template <int FMT, int RF, int CF, int SLOTS> struct MxTileShape {
-    static constexpr int ROWS = 64 * RF, COLS = 64 * CF, THREADS = 256;
+template <int FMT, int RF, int CF, int SLOTS, int KG> struct MxTileShape {
+    static constexpr int ROWS = 64 * RF, COLS = 64 * CF, THREADS = 256 * KG;
     static constexpr int COPIES = RF + CF;                          // 1 KiB copies per wave and half step: RF of 16 rows, CF of a weight block's 64 inputs
     static constexpr unsigned SLOT = (ROWS + COLS) * 64u, W_BASE = ROWS * 64u;
     static constexpr unsigned SCALES = FMT == MX_FP4 ? 4096u : 0u, S_BASE = SLOTS * SLOT;       // of a whole step, 1 KiB per wave: rows 0.., 128.., columns 0.., 128..; two of them
-    static constexpr unsigned LDS_BYTES = S_BASE + 2 * SCALES;
-    static constexpr int STORE_ROWS = RF % 2 == 0 && 2 * CF * 16384u <= LDS_BYTES ? 2 : 1;                   // rows of fragments per wave that mx_store leaves in LDS at a time
-    static_assert(STORE_ROWS * CF * 16384u <= LDS_BYTES, "four waves' fragments");
-    static constexpr int FIT = 163840 / LDS_BYTES, WAVES = RF * CF > 8 ? 1 : RF * CF > 2 ? 2 : FIT > 4 ? 4 : FIT;    // workgroups that a CU's LDS holds; waves per SIMD that registers are kept for
+    static constexpr unsigned GROUP = S_BASE + 2 * SCALES, LDS_BYTES = KG * GROUP;       // of a group of four waves
+    static_assert(LDS_BYTES <= 163840u && (KG == 1 || (RF % 2 == 0 && LDS_BYTES >= ROWS * COLS * 4u)), "what a CU has, and the groups' exchange");
+    static constexpr int STORE_ROWS = RF / KG % 2 == 0 && 2 * CF * 16384u <= GROUP ? 2 : 1;                   // rows of fragments per wave that mx_store leaves in LDS at a time
+    static_assert(STORE_ROWS * CF * 16384u <= GROUP, "four waves' fragments");
+    static constexpr int FIT = 163840 / LDS_BYTES, WAVES = RF * CF > 8 ? 1 : RF * CF > 2 || KG == 2 ? 2 : FIT > 4 ? 4 : FIT;    // workgroups that a CU's LDS holds; waves per SIMD that registers are kept for
     static constexpr int64_t PART_FLOATS = static_cast<int64_t>(ROWS) * COLS;
 };
 
@@ -141,12 +142,14 @@ __device__ __forceinline__ void mx_store_sums(float* sums, int splits, unsigned 
     }
 }
 
-template <int FMT, int RF, int CF, int SLOTS>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(MxTileShape<FMT, RF, CF, SLOTS>::WAVES)))
+template <int FMT, int RF, int CF, int SLOTS, int KG>
+__global__ void __launch_bounds__(256 * KG) __attribute__((amdgpu_waves_per_eu(MxTileShape<FMT, RF, CF, SLOTS, KG>::WAVES)))
 gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __restrict__ partial, int* __restrict__ arrived, GemmEpilogue ep) {
-    using T = MxTileShape<FMT, RF, CF, SLOTS>;
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<size_t>((__attribute__((address_space(3))) void*)(lds_raw)));
+    using T = MxTileShape<FMT, RF, CF, SLOTS, KG>;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_all[];
+    const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+    unsigned char* const lds_raw = lds_all + kg * T::GROUP;
+    const unsigned lds0 = static_cast<unsigned>(reinterpret_cast<size_t>((__attribute__((address_space(3))) void*)(lds_all))) + kg * T::GROUP;
     const int n_tiles = (p.n + T::COLS - 1) / T::COLS;
     const MxTiles<T::ROWS> row_tiles(p);
     const int m_tiles = row_tiles.total;
@@ -167,11 +170,16 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
     const MxTile t = row_tiles.find(p, m_tile);
     const int n0 = n_tile * T::COLS, n32 = (p.n + 31) & ~31;
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
     const int wm = wave >> 1, wn = wave & 1;
-    const int step0 = split * steps_per_split;
+    int step0 = split * steps_per_split;
     int n_steps = p.steps - step0;
     n_steps = n_steps < steps_per_split ? n_steps : steps_per_split;
+    const int n_turns = KG == 1 ? n_steps : (n_steps + 1) >> 1;                    // two groups: the first takes the first half of the steps, one more where they are odd
+    if (KG == 2) {
+        step0 += kg * n_turns;
+        n_steps = kg == 0 ? n_turns : n_steps - n_turns;
+    }
     const int n_half = 2 * n_steps;
 
     // Copy sources.  A: a lane copies 16 bytes of a row's 64; chunk c of row r lies at c ^ ((r >> 2) & 3), so that sixteen rows' same chunk covers all banks once.  Rows past the tensor's
@@ -328,9 +336,44 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
         for (int i = 0; i < RF; ++i) as[0][i] = as[1][i];
     }
     pp_wait<0>();                  // nothing may still be writing LDS when it is used again or the workgroup ends
+    if (KG == 2 && n_steps < n_turns) {       // the barriers of the other group's odd step
+        pp_barrier();
+        pp_barrier();
+    }
 
     const int m0 = t.row0 + wm * (RF * 32), n0w = n0 + wn * (CF * 32);
     if (ep.bias) ep.bias += static_cast<int64_t>(t.weight) * p.n;
+    if constexpr (KG == 2) {
+        // Each group leaves the half of its rows of fragments that the other one finishes, and adds what that one left of its own.
+        constexpr int H = RF / 2;
+        f32x4* const give = reinterpret_cast<f32x4*>(lds_all) + ((1 - kg) * 4 + wave) * (H * CF * 256) + lane;
+        const f32x4* const take = reinterpret_cast<const f32x4*>(lds_all) + (kg * 4 + wave) * (H * CF * 256) + lane;
+        auto finish = [&](auto first) __attribute__((always_inline)) {
+            constexpr int I0 = decltype(first)::value, G0 = H - I0;                // finishes rows [I0, I0 + H), gives [G0, G0 + H)
+            __syncthreads();
+#pragma unroll
+            for (int f = 0; f < H * CF; ++f) {
+                const f32x16 v = mx_here<false>(acc[G0 + f / CF][f % CF]);
+                give[f * 256] = mx_part<0>(v); give[f * 256 + 64] = mx_part<1>(v); give[f * 256 + 128] = mx_part<2>(v); give[f * 256 + 192] = mx_part<3>(v);
+            }
+            __syncthreads();
+            f32x16 sum[H][CF];
+#pragma unroll
+            for (int f = 0; f < H * CF; ++f)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const f32x4 x = take[f * 256 + c * 64];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[f / CF][f % CF][4 * c + e] = kg == 0 ? acc[I0 + f / CF][f % CF][4 * c + e] + x[e] : x[e] + acc[I0 + f / CF][f % CF][4 * c + e];
+                }
+            __syncthreads();
+            unsigned char* const own = lds_raw + wave * (T::STORE_ROWS * CF * 4096);
+            if (ep.vec_ok) mx_store<H, CF, T::STORE_ROWS, true>(sum, own, t, p.n, m0 + 32 * I0, n0w, ep);
+            else mx_store<H, CF, T::STORE_ROWS, false>(sum, own, t, p.n, m0 + 32 * I0, n0w, ep);
+        };
+        if (kg == 0) finish(zero{}); else finish(std::integral_constant<int, H>{});
+        return;
+    }
     if (splits > 1) {
         // As in pp_finish: every split leaves its sums in register order and the workgroup that arrives last adds all of them in split order.
         const int tile = n_tile * m_tiles + m_tile;
@@ -362,18 +405,19 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
     else mx_store<RF, CF, T::STORE_ROWS, false>(acc, own, t, p.n, m0, n0w, ep);
 }
 
-template <int FMT, int RF, int CF, int SLOTS>
+template <int FMT, int RF, int CF, int SLOTS, int KG>
 int launch_mx_tile(regione_ctx* ctx, const MxOperands& p, int splits, const GemmEpilogue& ep) {
-    using T = MxTileShape<FMT, RF, CF, SLOTS>;
+    using T = MxTileShape<FMT, RF, CF, SLOTS, KG>;
     static std::atomic<uint64_t> granted{0};
     const int64_t row_tiles = mx_most_row_tiles(p, T::ROWS), n_tiles = (p.n + T::COLS - 1) / T::COLS;
+    if (KG > 1) splits = 1;
     const int per = (p.steps + splits - 1) / splits, used = (p.steps + per - 1) / per;
     if (used > 1 && (static_cast<size_t>(row_tiles * n_tiles * used) * T::PART_FLOATS * sizeof(float) > ctx->gemm_part_bytes || row_tiles * n_tiles > kMaxSplitTiles))
         RG_FAIL(REGIONE_ERR_WORKSPACE, "linear: %d K-splits of a %d x %d result exceed the workspace", used, p.m, p.n);
     const int64_t workgroups = (row_tiles * n_tiles * used + 7) / 8 * 8;
     if (workgroups >= (int64_t{1} << 32) / T::THREADS) RG_FAIL(REGIONE_ERR_UNSUPPORTED, "linear: a result of %d x %d", p.m, p.n);
-    if (int rc = rg_grant_lds(ctx, reinterpret_cast<const void*>(gemm_mx_tile_kernel<FMT, RF, CF, SLOTS>), granted, T::LDS_BYTES)) return rc;
-    hipLaunchKernelGGL((gemm_mx_tile_kernel<FMT, RF, CF, SLOTS>), dim3(static_cast<unsigned>(workgroups)), dim3(T::THREADS), T::LDS_BYTES, ctx->stream, p, used, per, ctx->gemm_part, ctx->gemm_arrived, ep);
+    if (int rc = rg_grant_lds(ctx, reinterpret_cast<const void*>(gemm_mx_tile_kernel<FMT, RF, CF, SLOTS, KG>), granted, T::LDS_BYTES)) return rc;
+    hipLaunchKernelGGL((gemm_mx_tile_kernel<FMT, RF, CF, SLOTS, KG>), dim3(static_cast<unsigned>(workgroups)), dim3(T::THREADS), T::LDS_BYTES, ctx->stream, p, used, per, ctx->gemm_part, ctx->gemm_arrived, ep);
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }
@@ -381,17 +425,21 @@ int launch_mx_tile(regione_ctx* ctx, const MxOperands& p, int splits, const Gemm
 template <int FMT>
 int launch_mx_tile(regione_ctx* ctx, int tile, const MxOperands& p, int splits, const GemmEpilogue& ep) {
     switch (tile) {
-        case 44: return launch_mx_tile<FMT, 4, 4, 4>(ctx, p, splits, ep);
-        case 324: return launch_mx_tile<FMT, 2, 4, 3>(ctx, p, splits, ep);
-        case 342: return launch_mx_tile<FMT, 4, 2, 3>(ctx, p, splits, ep);
-        case 322: return launch_mx_tile<FMT, 2, 2, 3>(ctx, p, splits, ep);
-        case 34: return launch_mx_tile<FMT, 3, 4, 4>(ctx, p, splits, ep);
-        case 24: return launch_mx_tile<FMT, 2, 4, 4>(ctx, p, splits, ep);
-        case 42: return launch_mx_tile<FMT, 4, 2, 4>(ctx, p, splits, ep);
-        case 22: return launch_mx_tile<FMT, 2, 2, 4>(ctx, p, splits, ep);
-        case 12: return launch_mx_tile<FMT, 1, 2, 4>(ctx, p, splits, ep);
-        case 21: return launch_mx_tile<FMT, 2, 1, 4>(ctx, p, splits, ep);
-        case 11: return launch_mx_tile<FMT, 1, 1, 4>(ctx, p, splits, ep);
+        case 44: return launch_mx_tile<FMT, 4, 4, 4, 1>(ctx, p, splits, ep);
+        case 842: return launch_mx_tile<FMT, 4, 2, 3, 2>(ctx, p, splits, ep);
+        case 824: return launch_mx_tile<FMT, 2, 4, 3, 2>(ctx, p, splits, ep);
+        case 822: return launch_mx_tile<FMT, 2, 2, 4, 2>(ctx, p, splits, ep);
+        case 821: return launch_mx_tile<FMT, 2, 1, 4, 2>(ctx, p, splits, ep);
+        case 324: return launch_mx_tile<FMT, 2, 4, 3, 1>(ctx, p, splits, ep);
+        case 342: return launch_mx_tile<FMT, 4, 2, 3, 1>(ctx, p, splits, ep);
+        case 322: return launch_mx_tile<FMT, 2, 2, 3, 1>(ctx, p, splits, ep);
+        case 34: return launch_mx_tile<FMT, 3, 4, 4, 1>(ctx, p, splits, ep);
+        case 24: return launch_mx_tile<FMT, 2, 4, 4, 1>(ctx, p, splits, ep);
+        case 42: return launch_mx_tile<FMT, 4, 2, 4, 1>(ctx, p, splits, ep);
+        case 22: return launch_mx_tile<FMT, 2, 2, 4, 1>(ctx, p, splits, ep);
+        case 12: return launch_mx_tile<FMT, 1, 2, 4, 1>(ctx, p, splits, ep);
+        case 21: return launch_mx_tile<FMT, 2, 1, 4, 1>(ctx, p, splits, ep);
+        case 11: return launch_mx_tile<FMT, 1, 1, 4, 1>(ctx, p, splits, ep);
     }
     RG_FAIL(REGIONE_ERR_INVALID_ARG, "linear: no tile %d", tile);
 }
