@@ -21,7 +21,7 @@ struct MxPlan { int tile, splits; };      // tile 1, 2, 4, 8: the kernel of 16 r
 
 MxPlan choose(const MxOperands& p) {
     if (p.m <= 64) return {8, 1};
-    return {44, 1};
+    return {82, 1};
 }
 
 int launch(regione_ctx* ctx, int fmt, const MxOperands& p, const GemmEpilogue& ep) {
@@ -80,7 +80,7 @@ extern "C" int regione_linear_grouped(regione_ctx* ctx, const void* x, const voi
 extern "C" int regione_tune_mx(regione_ctx* ctx, int32_t tile, int32_t k_splits) {
     if (!ctx) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: null context");
     bool known = tile == 0;
-    for (int t : {1, 2, 4, 8, 842, 824, 822, 821, 44, 324, 342, 322, 34, 24, 42, 22, 12, 21, 11}) known = known || t == tile;
+    for (int t : {1, 2, 4, 8, 82, 62, 42, 81, 41, 22, 21, 11}) known = known || t == tile;
     if (!known || k_splits < 0 || k_splits > 16) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: no tile %d, or k_splits=%d is not in 0..16", tile, k_splits);
     ctx->mx_force_tile = tile;
     ctx->mx_force_splits = k_splits;
