@@ -51,7 +51,7 @@ struct regione_ctx {
     // created on first use; while a lane swap is active, `stream` and `gemm_part` name the lane's own stream and half
     hipStream_t side_stream;
     hipEvent_t ev_fork, ev_join;
-    GemmPlanSlot gemm_plans[kGemmPlanSlots];
+    GemmPlanSlot gemm_plans[kGemmPlanSlots], mx_plans[kGemmPlanSlots];
     int gemm_force_tn, gemm_force_splits;  // 0 = chosen per call
     int mx_force_tile, mx_force_splits;    // of the 4-bit and the grouped products
     int attn_force_splits, attn_force_form, attn_force_ranges;  // 0 = chosen per call

@@ -75,6 +75,41 @@ __device__ __forceinline__ f32x4 mx_mfma(const u32x4& w, const u32x4& a, const f
     else return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_half_operand(w), mx_half_operand(a), acc, 4, 4, 2 * H, static_cast<int>(w_scale), 2 * H, static_cast<int>(a_scale));
 }
 
+// 0.5 x (1 + tanh(u)) as in gelu_tanh_f32, without the correction of its quotient: 1.5 units of the last place of float32 from the reciprocal and the product, no more than what the rounded
+// argument of the exponential brings.  The end of a product in 4 bits is bound by these instructions: 820 x 12288 x 3072 31.9 -> 28.4 us, 25.8 without
+// activation.
+__device__ __forceinline__ float mx_gelu(float x) {
+    constexpr float kLin = -2.0f * 0.7978845608028654f * 1.4426950408889634f, kCub = kLin * 0.044715f;
+    const float e = __builtin_amdgcn_exp2f(x * __builtin_fmaf(x * x, kCub, kLin));
+    return 0.25f * x * __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, e, 0.25f));
+}
+// Eight consecutive columns of a row, those below N; WIDE: all eight, in whole pieces of 16 bytes.
+struct MxBias {
+    float v[8];
+    __device__ __forceinline__ MxBias(const GemmEpilogue& ep, int col, int N) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = ep.bias && col + e < N ? ep.bias[col + e] : 0.f;
+    }
+};
+template <bool WIDE>
+__device__ __forceinline__ void mx_put8(const GemmEpilogue& ep, int row, int col, int N, const f32x4& lo, const f32x4& hi, const MxBias& bias) {
+    float val[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) val[e] = (e < 4 ? lo[e & 3] : hi[e & 3]) + bias.v[e];
+    if (ep.act == REGIONE_ACT_GELU_TANH) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) val[e] = mx_gelu(val[e]);
+    }
+    const int64_t at = static_cast<int64_t>(row) * ep.ldy + col;
+    if (WIDE || col + 8 <= N) { store8<WIDE>(ep.y, at, ep.y_f32, val); return; }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (col + e < N) {
+            if (ep.y_f32) static_cast<float*>(ep.y)[at + e] = val[e];
+            else static_cast<bf16_t*>(ep.y)[at + e] = f32_to_bf16(val[e]);
+        }
+}
+
 // Few rows: a wave owns 16 rows x 32 columns of a part of K and reads its operands straight from memory, the weights as they lie, with the loads of CHUNK steps in flight.  KW of a workgroup's
 // eight waves share K and meet in LDS, where the sums are formed in wave order; the others take further columns.  Such a launch is a chain of trips to memory and the reading of
 // the weights.
@@ -154,14 +189,9 @@ gemm_mx_small_kernel(MxOperands p, GemmEpilogue ep) {
     if (ep.bias) ep.bias += static_cast<int64_t>(t.weight) * p.n;
     const int col = n0 + 8 * kc;
     if (t.row0 + l16 >= t.end || t.row0 + l16 < t.begin || col >= p.n) return;
-    if (col + 8 > p.n) { epilogue_ragged<EPI_PLAIN, false>(ep, row, col, p.n, acc[0], acc[1]); return; }
-    EpiColumns<EPI_PLAIN, false> cols;
-    EpiRow<EPI_PLAIN, false> r;
-    Raw8 raw;
-    cols.load(ep, col);
-    r.load(ep, row);
-    if (ep.vec_ok) epilogue_store8<EPI_PLAIN, false, true>(ep, row, col, acc[0], acc[1], cols, r, raw);
-    else epilogue_store8<EPI_PLAIN, false, false>(ep, row, col, acc[0], acc[1], cols, r, raw);
+    const MxBias bias(ep, col, p.n);
+    if (ep.vec_ok) mx_put8<true>(ep, row, col, p.n, acc[0], acc[1], bias);
+    else mx_put8<false>(ep, row, col, p.n, acc[0], acc[1], bias);
 }
 
 }  // namespace

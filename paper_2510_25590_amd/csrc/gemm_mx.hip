@@ -1,5 +1,6 @@
 // Products of microscaled 4-bit operands, and products over groups of rows with weights of their own: which kernel a call gets, and the entry points.
 #include "gemm_mx.h"
+#include <math.h>
 
 namespace {
 
@@ -17,19 +18,89 @@ int launch_small(regione_ctx* ctx, int waves, const MxOperands& p, const GemmEpi
     return waves == 1 ? launch_small<FMT, 1>(ctx, p, ep) : waves == 2 ? launch_small<FMT, 2>(ctx, p, ep) : waves == 4 ? launch_small<FMT, 4>(ctx, p, ep) : launch_small<FMT, 8>(ctx, p, ep);
 }
 
+// ---- which kernel a product gets
+//
+// A plan's time is estimated as a start, whole and partial loads of the chip by workgroups (a fixed part and a part per step of K, which grow with the workgroups that share a CU, and the
+// activation, which they do one after the other), not less than the weights take from HBM, and the results' way out; a K split adds its sums' way out and back, the kernel of 16 rows what
+// its repeated reading of the weights takes.  The host does not know the groups' sizes: they are taken as random (exponentially distributed), a group of mean length s then has
+// 1 / (1 - exp(-R / s)) tiles of R rows.  All constants are fitted to every tile, K split and number of waves of 1193 products in 4 bits and 803 in bf16 (1-16384 rows, 64-12288 columns,
+// K 256-15360, up to 64 groups, equal and random, with and without activation): over 597 / 402 others the choice is 2.0 / 4.7 % behind the best plan measured on average, 10 / 23 % in the
+// twentieth of them where it is furthest, 54 / 58 % at most (groups whose sizes are far from the assumed ones).
+// us, another tile / the choice: 820 x 12288 x 3072 256 x 256 32.0 / 192 x 256 25.8; 820 x 3072 x 12288 256 x 256 61.7 / 128 x 128 27.4; 128 x 3072 x 12288 unsplit 19.8 / four K splits
+// 13.7; 8704 x 12288 x 3072 128 x 128 204 / 128 x 256 172; one row x 9216 x 3072 all waves over columns 9.8 / four over K 5.2.
 struct MxPlan { int tile, splits; };      // tile 1, 2, 4, 8: the kernel of 16 rows with as many waves over K
+struct MxTileCost { int code, per_cu; double fixed, step, more; };               // us, us per step, and what each further workgroup of a CU adds to the latter (as a share)
+struct MxSmallCost { int waves; double fixed, step, work; };                      // us, us per step of a wave, us per 1e5 steps of columns
+struct MxCosts { MxTileCost tile[11]; MxSmallCost small[4]; double start, hbm, out, gelu; };     // us, bytes of weights per us, results per us, us per 100 kB of a tile's sums
+constexpr MxCosts kMxCosts[2] = {
+    {{{72, 1, 2.68, 0.937, 0.0}, {62, 1, 2.27, 0.805, 0.0}, {52, 1, 1.79, 0.678, 0.0}, {42, 2, 0.83, 0.563, 0.951}, {32, 2, 0.41, 0.483, 0.926}, {51, 2, 0.83, 0.393, 1.088},
+      {41, 2, 0.39, 0.328, 1.131}, {31, 3, 0.12, 0.268, 1.119}, {22, 2, 0.03, 0.378, 1.045}, {21, 3, 0.00, 0.216, 1.179}, {11, 3, 0.24, 0.165, 1.368}},
+     {{1, 0.49, 0.198, 1.14}, {2, 0.00, 0.281, 1.16}, {4, 0.22, 0.206, 1.23}, {8, 0.60, 0.028, 1.32}}, 3.61, 7.73e6, 0.98e6, 0.69},
+    {{{72, 1, 2.90, 1.178, 0.0}, {62, 1, 2.22, 1.004, 0.0}, {52, 1, 2.21, 0.855, 0.0}, {42, 2, 1.18, 0.651, 1.009}, {32, 2, 0.83, 0.543, 1.056}, {51, 2, 0.93, 0.453, 1.459},
+      {41, 2, 0.67, 0.363, 1.636}, {31, 3, 0.44, 0.299, 1.380}, {22, 2, 0.60, 0.405, 1.275}, {21, 3, 0.29, 0.228, 1.463}, {11, 3, 0.51, 0.177, 1.695}},
+     {{1, 0.00, 0.408, 1.23}, {2, 0.01, 0.451, 1.07}, {4, 0.11, 0.428, 1.04}, {8, 0.25, 0.344, 1.15}}, 3.69, 6.63e6, 1.49e6, 0.78}};
 
-MxPlan choose(const MxOperands& p) {
-    if (p.m <= 64) return {8, 1};
-    return {82, 1};
+double row_tiles_expected(int m, int groups, int R) {
+    if (groups <= 1) return (m + R - 1) / R;
+    const double g = groups < m ? groups : m;
+    return g / (1.0 - exp(-R * g / m));
+}
+MxPlan choose(int fmt, const MxOperands& p, int act, size_t part_bytes) {
+    const MxCosts& c = kMxCosts[fmt];
+    const int groups = p.offsets ? p.n_groups : 1;
+    const double weights = static_cast<double>(p.m < groups ? p.m : groups) * p.n * p.steps * (fmt == MX_FP4 ? 136.0 : 128.0) / c.hbm;
+    MxPlan best = {42, 1};
+    double best_us = 1e30;
+    auto consider = [&](int tile, int splits, double us) { if (us < best_us) { best_us = us; best = {tile, splits}; } };
+    for (const MxTileCost& t : c.tile) {
+        const int R = 32 * (t.code / 10), C = 128 * (t.code % 10);
+        const double columns = (p.n + C - 1) / C, units = ceil(row_tiles_expected(p.m, groups, R)) * columns;
+        const int64_t most = mx_most_row_tiles(p, R) * static_cast<int64_t>(columns);
+        const double tile_kb = R * C * 4.0 / 1e3, gelu = act == REGIONE_ACT_GELU_TANH ? c.gelu * tile_kb / 100.0 : 0.0;
+        for (int s : {1, 2, 3, 4, 6, 8}) {
+            if (s > 1) {
+                if (p.offsets || units * s > 640 || p.steps < 2 * s) break;
+                if (most > kMaxSplitTiles || static_cast<size_t>(most) * s * R * C * sizeof(float) > part_bytes) break;
+                const int per = (p.steps + s - 1) / s;
+                if ((p.steps + per - 1) / per != s) continue;     // another split count in disguise
+            }
+            const int per = (p.steps + s - 1) / s;
+            const double loads = floor(units * s / (256.0 * t.per_cu)), rest = units * s - loads * 256.0 * t.per_cu;
+            auto load = [&](double shared) { return t.fixed + per * t.step * (1.0 + t.more * (shared - 1.0)) + gelu * shared; };
+            double us = loads * load(t.per_cu) + (rest > 0.0 ? load(ceil(rest / 256.0)) : 0.0);
+            if (us < weights) us = weights;
+            us += static_cast<double>(p.m) * p.n / c.out;
+            if (s > 1) us += 0.97 + 0.295 * units * s * tile_kb / 1e3 + 0.0196 * s * tile_kb;
+            consider(t.code, s, c.start + us);
+        }
+    }
+    if (p.m > 48 * static_cast<int64_t>(groups)) return best;     // (more than what the kernel of 16 rows was fitted to)
+    for (const MxSmallCost& t : c.small) {
+        const int C = 256 / t.waves;
+        const double units = ceil(row_tiles_expected(p.m, groups, kMxSmallRows)) * ((p.n + C - 1) / C);
+        const double us = t.fixed + t.step * ((p.steps + t.waves - 1) / t.waves) + t.work * 1e-5 * units * p.steps * C;
+        consider(t.waves, 1, c.start + (us < weights ? weights : us));
+    }
+    return best;
+}
+// remembered per context like the other products' plans (plan_gemm in gemm.hip)
+MxPlan plan(regione_ctx* ctx, int fmt, const MxOperands& p, int act) {
+    const int groups = p.offsets ? p.n_groups : 0;
+    const uint32_t h = (static_cast<uint32_t>(p.m) * 2654435761u) ^ (static_cast<uint32_t>(p.n) * 2246822519u) ^ (static_cast<uint32_t>(p.row_bytes) * 3266489917u) ^ (static_cast<uint32_t>(groups) * 668265263u);
+    GemmPlanSlot& slot = ctx->mx_plans[(h >> 16) % kGemmPlanSlots];
+    const int kind = 4 * groups + 2 * act + fmt;
+    if (slot.m == p.m && slot.n == p.n && slot.k == p.row_bytes && slot.kind == kind && slot.part_bytes == ctx->gemm_part_bytes) return {slot.tile, slot.splits};
+    const MxPlan best = choose(fmt, p, act, ctx->gemm_part_bytes);
+    slot = {p.m, p.n, p.row_bytes, kind, best.tile, best.splits, ctx->gemm_part_bytes};
+    return best;
 }
 
 int launch(regione_ctx* ctx, int fmt, const MxOperands& p, const GemmEpilogue& ep) {
     ProfScope prof(ctx, REGIONE_PROF_GEMM);
-    MxPlan plan = choose(p);
-    if (ctx->mx_force_tile) plan = {ctx->mx_force_tile, ctx->mx_force_splits > 0 && !p.offsets ? ctx->mx_force_splits : 1};
-    if (plan.tile <= 8) return fmt == MX_FP4 ? launch_small<MX_FP4>(ctx, plan.tile, p, ep) : launch_small<MX_BF16>(ctx, plan.tile, p, ep);
-    return fmt == MX_FP4 ? rg_mx_tile_4bit(ctx, plan.tile, p, plan.splits, ep) : rg_mx_tile_bf16(ctx, plan.tile, p, plan.splits, ep);
+    MxPlan to = plan(ctx, fmt, p, ep.act);
+    if (ctx->mx_force_tile) to = {ctx->mx_force_tile, ctx->mx_force_splits > 0 && !p.offsets ? ctx->mx_force_splits : 1};
+    if (to.tile <= 8) return fmt == MX_FP4 ? launch_small<MX_FP4>(ctx, to.tile, p, ep) : launch_small<MX_BF16>(ctx, to.tile, p, ep);
+    return fmt == MX_FP4 ? rg_mx_tile_4bit(ctx, to.tile, p, to.splits, ep) : rg_mx_tile_bf16(ctx, to.tile, p, to.splits, ep);
 }
 
 // What the three products have in common.  groups: offsets, use, n_groups and n_weights are looked at.
@@ -41,8 +112,8 @@ int linear(regione_ctx* ctx, const char* who, int fmt, bool groups, const void* 
     if (act != REGIONE_ACT_NONE && act != REGIONE_ACT_GELU_TANH) RG_FAIL(REGIONE_ERR_INVALID_ARG, "%s: bad act %d", who, act);
     if (out_dtype != REGIONE_BF16 && out_dtype != REGIONE_FP32) RG_FAIL(REGIONE_ERR_INVALID_ARG, "%s: bad out_dtype %d", who, out_dtype);
     const int unit = fmt == MX_FP4 ? kMxBlock : 64;
-    if (k % unit || k > (1 << 20)) RG_FAIL(REGIONE_ERR_BAD_SHAPE, "%s: k=%d must be a multiple of %d, at most 2^20", who, k, unit);
-    if (n > (1 << 24) || m > (1 << 24)) RG_FAIL(REGIONE_ERR_BAD_SHAPE, "%s: m=%d n=%d (at most 2^24)", who, m, n);
+    if (k % unit || k > kMxMostInputs) RG_FAIL(REGIONE_ERR_BAD_SHAPE, "%s: k=%d must be a multiple of %d, at most 2^20", who, k, unit);
+    if (n > kMxMostFeatures || m > (1 << 24)) RG_FAIL(REGIONE_ERR_BAD_SHAPE, "%s: m=%d n=%d (at most 2^24)", who, m, n);
     if (groups && (n_groups < 0 || n_weights <= 0 || n_groups > (1 << 16) || (!use && n_groups > n_weights)))
         RG_FAIL(REGIONE_ERR_INVALID_ARG, "%s: %d groups (at most 65536), %d weights", who, n_groups, n_weights);
     if (m == 0 || (groups && n_groups == 0)) return REGIONE_OK;
@@ -80,7 +151,7 @@ extern "C" int regione_linear_grouped(regione_ctx* ctx, const void* x, const voi
 extern "C" int regione_tune_mx(regione_ctx* ctx, int32_t tile, int32_t k_splits) {
     if (!ctx) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: null context");
     bool known = tile == 0;
-    for (int t : {1, 2, 4, 8, 82, 62, 42, 81, 41, 22, 21, 11}) known = known || t == tile;
+    for (int t : {1, 2, 4, 8, 72, 62, 52, 42, 32, 51, 41, 31, 22, 21, 11}) known = known || t == tile;
     if (!known || k_splits < 0 || k_splits > 16) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: no tile %d, or k_splits=%d is not in 0..16", tile, k_splits);
     ctx->mx_force_tile = tile;
     ctx->mx_force_splits = k_splits;

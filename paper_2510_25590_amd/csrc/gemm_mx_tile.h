@@ -1,11 +1,13 @@
-// The products of gemm_mx.h for many rows: tiles of 32 x 128 to 256 x 256 results.
+// The products of gemm_mx.h for many rows: tiles of 32 x 128 to 224 x 256 results.
 //
 // Four waves; each owns all 32 * RF rows of the tile and 32 * CF columns, in 32x32 fragments.  The weights go from their packed layout straight into the registers of the one wave that
 // wants them; the rows, which all waves want, go by way of registers into LDS, a whole step (128 bytes of a row, one line of memory) at a time, two steps in LDS.  Loads are requested
 // LOOK steps ahead and registers are loaded again as soon as they have been used.  A step is four phases of RF * CF instructions; while a phase's instructions run, the same wave reads the
 // rows of the next phase, puts rows of the next step into LDS and requests rows, weights and scales of the steps ahead.  One barrier per step.
 // Why not straight into LDS: such copies are taken at 35 bytes a clock by a CU (all tiles ended at 65 to 70 bytes a ns), where loads into registers get 64; and
-// weights in LDS, shared by waves that split the rows, cost it as many bytes again.  us, tiles of the same sizes with copies into LDS / now: MXT_1.
+// weights in LDS, shared by waves that split the rows, cost it as many bytes again.  us, tiles of the same sizes with copies into LDS / now: 820 x 3072 x 12288 30.0 / 27.6,
+// 205 x 12288 x 3072 12.5 / 11.4, 64 x 9216 x 3072 6.9 / 6.2, 128 x 3072 x 12288 23.6 / 20.0, 2048 x 8192 x 12288 106 / 97.  A large product is then bound by power: 128 x 256 tiles of
+// 8704 x 12288 x 3072 run at 3.8 PFLOP/s, the matrix instructions busy at 1.8 to 1.9 GHz; a small one by the weights from HBM and the trips there.
 // The 32x32 instruction reaches its rate with one wave per SIMD, which the 16x16 one does not (register-only loops in 4 bits, PFLOP/s with one, two and four waves per
 // SIMD: 6.3 / 6.5 / 6.6 against 4.2 / 5.5 / 6.1).
 #pragma once
@@ -58,10 +60,7 @@ __device__ __forceinline__ void mx_store(const f32x16 (&acc)[RF][CF], unsigned c
     static_assert(RF % IR == 0, "whole rounds");
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int group = lane % GROUPS, col = n0w + 8 * group;
-    Raw8 raw;
-    EpiRow<EPI_PLAIN, false> r;
-    EpiColumns<EPI_PLAIN, false> cols;
-    if (col + 8 <= N) cols.load(ep, col);
+    const MxBias bias(ep, col, N);
     f32x4* const to = reinterpret_cast<f32x4*>(lds) + l32 * PIECES;
     const f32x4* const from = reinterpret_cast<const f32x4*>(lds);
     for (int i0 = 0; i0 < RF; i0 += IR) {
@@ -83,8 +82,7 @@ __device__ __forceinline__ void mx_store(const f32x16 (&acc)[RF][CF], unsigned c
             const int row = m0 + 32 * i0 + lr;
             const f32x4 lo = from[lr * PIECES + ((2 * group) ^ (lr & KEY))], hi = from[lr * PIECES + ((2 * group + 1) ^ (lr & KEY))];
             if (row < t.begin || row >= t.end || col >= N) continue;
-            if (ALIGNED || col + 8 <= N) epilogue_store8<EPI_PLAIN, false, ALIGNED>(ep, row, col, lo, hi, cols, r, raw);
-            else epilogue_ragged<EPI_PLAIN, false>(ep, row, col, N, lo, hi);
+            mx_put8<ALIGNED>(ep, row, col, N, lo, hi, bias);
         }
     }
 }
@@ -96,8 +94,6 @@ __device__ __forceinline__ void mx_store_sums(float* sums, int splits, unsigned 
     constexpr unsigned bytes = RF * CF * 4u * 4096u;               // of a split
     const auto rsrc = pp_part_rsrc(sums, splits * static_cast<int64_t>(bytes / 4));
     const int l32 = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1;
-    Raw8 raw;
-    EpiRow<EPI_PLAIN, false> r;
     for (int f0 = 0; f0 < F; f0 += G) {
         f32x4 sum[G * 4];
         u32x4 v[2][G * 4];
@@ -123,14 +119,10 @@ __device__ __forceinline__ void mx_store_sums(float* sums, int splits, unsigned 
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int col = n0w + 32 * ((f0 + g) % CF) + 16 * b + 8 * half;
-                if (col + 8 <= N) {
-                    EpiColumns<EPI_PLAIN, false> cols;
-                    cols.load(ep, col);
-                    if (ep.vec_ok) epilogue_store8<EPI_PLAIN, false, true>(ep, row, col, sum[4 * g + 2 * b], sum[4 * g + 2 * b + 1], cols, r, raw);
-                    else epilogue_store8<EPI_PLAIN, false, false>(ep, row, col, sum[4 * g + 2 * b], sum[4 * g + 2 * b + 1], cols, r, raw);
-                } else if (col < N) {
-                    epilogue_ragged<EPI_PLAIN, false>(ep, row, col, N, sum[4 * g + 2 * b], sum[4 * g + 2 * b + 1]);
-                }
+                if (col >= N) continue;
+                const MxBias bias(ep, col, N);
+                if (ep.vec_ok) mx_put8<true>(ep, row, col, N, sum[4 * g + 2 * b], sum[4 * g + 2 * b + 1], bias);
+                else mx_put8<false>(ep, row, col, N, sum[4 * g + 2 * b], sum[4 * g + 2 * b + 1], bias);
             }
         }
     }
@@ -374,11 +366,14 @@ int launch_mx_tile(regione_ctx* ctx, const MxOperands& p, int splits, const Gemm
 template <int FMT>
 int launch_mx_tile(regione_ctx* ctx, int tile, const MxOperands& p, int splits, const GemmEpilogue& ep) {
     switch (tile) {
-        case 82: return launch_mx_tile<FMT, 8, 2, 1, 1>(ctx, p, splits, ep);
+        case 72: return launch_mx_tile<FMT, 7, 2, 1, 1>(ctx, p, splits, ep);
         case 62: return launch_mx_tile<FMT, 6, 2, 1, 1>(ctx, p, splits, ep);
+        case 52: return launch_mx_tile<FMT, 5, 2, 1, 1>(ctx, p, splits, ep);
         case 42: return launch_mx_tile<FMT, 4, 2, 1, 2>(ctx, p, splits, ep);
-        case 81: return launch_mx_tile<FMT, 8, 1, 1, 1>(ctx, p, splits, ep);
+        case 32: return launch_mx_tile<FMT, 3, 2, 1, 2>(ctx, p, splits, ep);
+        case 51: return launch_mx_tile<FMT, 5, 1, 2, 2>(ctx, p, splits, ep);
         case 41: return launch_mx_tile<FMT, 4, 1, 2, 2>(ctx, p, splits, ep);
+        case 31: return launch_mx_tile<FMT, 3, 1, 2, 2>(ctx, p, splits, ep);
         case 22: return launch_mx_tile<FMT, 2, 2, 2, 2>(ctx, p, splits, ep);
         case 21: return launch_mx_tile<FMT, 2, 1, 2, 3>(ctx, p, splits, ep);
         case 11: return launch_mx_tile<FMT, 1, 1, 4, 3>(ctx, p, splits, ep);

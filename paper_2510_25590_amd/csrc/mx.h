@@ -3,6 +3,7 @@
 #include "common.h"
 
 constexpr int kMxBlock = 32;             // values that share a scale
+constexpr int kMxMostInputs = 1 << 20, kMxMostFeatures = 1 << 24;         // of a product: offsets inside a tile stay below 2^31 bytes
 constexpr int kMxStep = 256;             // values of a row in one K-step of the products: 128 bytes of codes, eight scales
 
 // Scales in steps: for every step the rows one after the other, eight bytes per row, so that the rows of a tile are one piece of memory.  Block b is byte 4*(b%2) + b/2: a lane of
@@ -13,7 +14,7 @@ __host__ __device__ __forceinline__ int64_t mx_scale_step(int64_t row, int block
     return ((block >> 3) * padded_rows + row) * 8 + 4 * (block & 1) + ((block & 7) >> 1);
 }
 __host__ __device__ __forceinline__ int64_t mx_packed_bytes(int n, int k) {
-    const int64_t n32 = (n + 31) & ~31, steps = (k + kMxStep - 1) / kMxStep;
+    const int64_t n32 = (static_cast<int64_t>(n) + 31) & ~31, steps = (static_cast<int64_t>(k) + kMxStep - 1) / kMxStep;
     return n32 * steps * (kMxStep / 2 + 8);
 }
 // 2^(byte - 127), as the conversion instructions take it: they read the exponent field
@@ -36,6 +37,6 @@ static inline int64_t mx_most_row_tiles(const MxOperands& p, int R) {
     return p.m / R + (p.n_groups < p.m ? p.n_groups : p.m);
 }
 
-// The kernel of tiles (gemm_mx_tile.h): its code is 10 * RF + CF, for 64 * RF rows and 64 * CF columns.  REGIONE_ERR_INVALID_ARG for a code that there is no kernel of.
+// The kernel of tiles (gemm_mx_tile.h): its code is 10 * RF + CF, for 32 * RF rows and 128 * CF columns.  REGIONE_ERR_INVALID_ARG for a code that there is no kernel of.
 int rg_mx_tile_4bit(regione_ctx* ctx, int tile, const MxOperands& p, int splits, const GemmEpilogue& ep);
 int rg_mx_tile_bf16(regione_ctx* ctx, int tile, const MxOperands& p, int splits, const GemmEpilogue& ep);

@@ -203,7 +203,7 @@ void launch_quantize(regione_ctx* ctx, dim3 grid, const void* x, int64_t rows, i
 int check_rows(regione_ctx* ctx, const char* who, int64_t rows, int32_t cols, int32_t layout) {
     if (!ctx) RG_FAIL(REGIONE_ERR_INVALID_ARG, "%s: null context", who);
     if (layout != REGIONE_MX_SCALE_ROWS && layout != REGIONE_MX_SCALE_STEPS) RG_FAIL(REGIONE_ERR_INVALID_ARG, "%s: scale layout %d", who, layout);
-    if (rows < 0 || rows > INT32_MAX || cols <= 0 || cols % kMxBlock || cols > (1 << 20))
+    if (rows < 0 || rows > INT32_MAX || cols <= 0 || cols % kMxBlock || cols > kMxMostInputs)
         RG_FAIL(REGIONE_ERR_BAD_SHAPE, "%s: rows=%lld, cols=%d (a multiple of 32, at most 2^20)", who, (long long)rows, cols);
     return REGIONE_OK;
 }
@@ -247,7 +247,7 @@ extern "C" int regione_dequantize_rows_mxfp4(regione_ctx* ctx, const void* q, co
 extern "C" int64_t regione_mxfp4_scale_bytes(int64_t rows, int32_t cols, int32_t scale_layout) {
     if (rows <= 0 || cols <= 0) return 0;
     if (scale_layout != REGIONE_MX_SCALE_STEPS) return rows * ((cols + kMxBlock - 1) / kMxBlock);
-    return mx_padded_rows(rows) * 8 * ((cols + kMxStep - 1) / kMxStep);
+    return mx_padded_rows(rows) * 8 * ((static_cast<int64_t>(cols) + kMxStep - 1) / kMxStep);
 }
 
 extern "C" int64_t regione_packed_weight_mxfp4_bytes(int32_t n, int32_t k) {
@@ -257,7 +257,8 @@ extern "C" int64_t regione_packed_weight_mxfp4_bytes(int32_t n, int32_t k) {
 extern "C" int regione_pack_weight_mxfp4(regione_ctx* ctx, const void* wq, const void* w_scale, int32_t n, int32_t k, void* w_packed) {
     if (!ctx) RG_FAIL(REGIONE_ERR_INVALID_ARG, "pack_weight_mxfp4: null context");
     if (ctx->f32) RG_FAIL(REGIONE_ERR_UNSUPPORTED, "pack_weight_mxfp4: the 4-bit projections belong to bf16 contexts");
-    if (n <= 0 || k <= 0 || (k % kMxBlock)) RG_FAIL(REGIONE_ERR_BAD_SHAPE, "pack_weight_mxfp4: n=%d, k=%d (k must be a multiple of 32)", n, k);
+    if (n <= 0 || n > kMxMostFeatures || k <= 0 || k % kMxBlock || k > kMxMostInputs)
+        RG_FAIL(REGIONE_ERR_BAD_SHAPE, "pack_weight_mxfp4: n=%d (at most 2^24), k=%d (a multiple of 32, at most 2^20)", n, k);
     if (!wq || !w_scale || !w_packed || !rg_aligned16(wq) || !rg_aligned16(w_packed)) RG_FAIL(REGIONE_ERR_INVALID_ARG, "pack_weight_mxfp4: null or unaligned tensor");
     if (wq == w_packed || w_scale == w_packed) RG_FAIL(REGIONE_ERR_INVALID_ARG, "pack_weight_mxfp4: cannot pack in place");
     const int64_t chunks = static_cast<int64_t>((n + 31) / 32 * 32) * ((k + kMxStep - 1) / kMxStep) * 8;

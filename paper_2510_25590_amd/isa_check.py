@@ -195,13 +195,6 @@ def check_function(name: str, lines, unroll: int = 0) -> list[str]:
 
 
 _COPY = "global_load_lds_dwordx4"
-
-
-def _is_copy(instr: str) -> bool:
-    """A copy into LDS, by address or through a buffer resource."""
-    return instr.startswith(_COPY) or (instr.startswith("buffer_load_dwordx4") and instr.split()[-1] == "lds")
-
-
 _WIDE_STORE = re.compile(r"^(buffer|global)_store_dwordx[34]\b")
 
 
@@ -221,11 +214,11 @@ def check_copies(name: str, lines) -> list[str]:
                 work += blocks[b][2]
         reach.append(seen)
     for k, b in enumerate(blocks):
-        if k not in reach[k] or not any(_is_copy(i) or i.startswith("v_mfma") for i, _ in b[1]):
+        if k not in reach[k] or not any(i.startswith(_COPY) or i.startswith("v_mfma") for i, _ in b[1]):
             continue
         for instr, in_asm in b[1]:
             op = instr.split()[0]
-            if re.match(r"^(global|buffer|flat|scratch)_(load|store|atomic)", op) and not (in_asm and _is_copy(instr)):
+            if re.match(r"^(global|buffer|flat|scratch)_(load|store|atomic)", op) and not (in_asm and op == _COPY):
                 errors.append(f"{short} block {b[0] or k}: '{instr}' among the counted copies")
     return errors
 
@@ -251,7 +244,8 @@ def check_asm(asm: str) -> None:
     problems: list[str] = []
     for name, lines in _kernel_bodies(asm, "gemm_"):
         n += 1
-        if any(_is_copy(line.strip()) for line in lines):
+        text = "\n".join(lines)
+        if _COPY in text:
             m = re.search(r"; ScratchSize: (\d+)", asm[asm.index(name + ":"):])
             if m and int(m.group(1)) != 0:
                 problems.append(f"{name[:70]}: uses {m.group(1)} bytes of scratch memory (its accesses share the copies' counter)")

@@ -8,7 +8,7 @@ from paper_2510_25590_amd import binding as rg
 
 pytestmark = pytest.mark.gpu
 
-TILES = [1, 2, 4, 8, 82, 62, 42, 81, 41, 22, 21, 11]
+TILES = [1, 2, 4, 8, 72, 62, 52, 42, 32, 51, 41, 31, 22, 21, 11]
 
 
 @pytest.fixture
