@@ -40,10 +40,11 @@ constexpr MxCosts kMxCosts[2] = {
       {41, 2, 0.67, 0.363, 1.636}, {31, 3, 0.44, 0.299, 1.380}, {22, 2, 0.60, 0.405, 1.275}, {21, 3, 0.29, 0.228, 1.463}, {11, 3, 0.51, 0.177, 1.695}},
      {{1, 0.00, 0.408, 1.23}, {2, 0.01, 0.451, 1.07}, {4, 0.11, 0.428, 1.04}, {8, 0.25, 0.344, 1.15}}, 3.69, 6.63e6, 1.49e6, 0.78}};
 
-double row_tiles_expected(int m, int groups, int R) {
-    if (groups <= 1) return (m + R - 1) / R;
-    const double g = groups < m ? groups : m;
-    return g / (1.0 - exp(-R * g / m));
+double row_tiles_expected(const MxOperands& p, int R) {
+    const double most = static_cast<double>(mx_most_row_tiles(p, R)), g = p.n_groups < p.m ? p.n_groups : p.m;
+    if (!p.offsets) return most;
+    const double random = ceil(g / (1.0 - exp(-R * g / p.m)));
+    return random < most ? random : most;
 }
 MxPlan choose(int fmt, const MxOperands& p, int act, size_t part_bytes) {
     const MxCosts& c = kMxCosts[fmt];
@@ -54,7 +55,7 @@ MxPlan choose(int fmt, const MxOperands& p, int act, size_t part_bytes) {
     auto consider = [&](int tile, int splits, double us) { if (us < best_us) { best_us = us; best = {tile, splits}; } };
     for (const MxTileCost& t : c.tile) {
         const int R = 32 * (t.code / 10), C = 128 * (t.code % 10);
-        const double columns = (p.n + C - 1) / C, units = ceil(row_tiles_expected(p.m, groups, R)) * columns;
+        const double columns = (p.n + C - 1) / C, units = row_tiles_expected(p, R) * columns;
         const int64_t most = mx_most_row_tiles(p, R) * static_cast<int64_t>(columns);
         const double tile_kb = R * C * 4.0 / 1e3, gelu = act == REGIONE_ACT_GELU_TANH ? c.gelu * tile_kb / 100.0 : 0.0;
         for (int s : {1, 2, 3, 4, 6, 8}) {
@@ -77,7 +78,7 @@ MxPlan choose(int fmt, const MxOperands& p, int act, size_t part_bytes) {
     if (p.m > 48 * static_cast<int64_t>(groups)) return best;     // (more than what the kernel of 16 rows was fitted to)
     for (const MxSmallCost& t : c.small) {
         const int C = 256 / t.waves;
-        const double units = ceil(row_tiles_expected(p.m, groups, kMxSmallRows)) * ((p.n + C - 1) / C);
+        const double units = row_tiles_expected(p, kMxSmallRows) * ((p.n + C - 1) / C);
         const double us = t.fixed + t.step * ((p.steps + t.waves - 1) / t.waves) + t.work * 1e-5 * units * p.steps * C;
         consider(t.waves, 1, c.start + (us < weights ? weights : us));
     }

@@ -51,18 +51,32 @@ template <bool ACC_REGISTERS> __device__ __forceinline__ f32x16 mx_here(f32x16 v
 }
 
 // Writes a wave's accumulators: acc[i][j] of a lane holds row 32*i + lane%32 and columns 32*j + 16*b + 8*(lane/32) + 0..7, b = 0, 1, of the wave's part.  By way of LDS (the wave's own
-// part of it, IR rows of fragments at a time), so that a store covers whole rows of the part, 256 bytes at 128 bf16 columns: straight from the accumulators, 32 bytes of 32
+// part of it, IR rows of fragments at a time), so that a store covers whole rows of the part, 16 bytes per lane: straight from the accumulators, 32 bytes of 32
 // rows at a time, 2048 x 8192 x 256 took 17.6 us instead of 15.1.
+template <int ROWS, int CF, int E, bool ALIGNED>                                  // E columns per lane: eight of bf16, four of float32
+__device__ __forceinline__ void mx_store_rows(const unsigned char* lds, const MxTile& t, int N, int row0, int col, const GemmEpilogue& ep, const MxBias& bias) {
+    constexpr int PIECES = 8 * CF, KEY = (PIECES < 16 ? PIECES : 16) - 1;        // 16-byte pieces of a row; piece c of row r lies at c ^ (r & KEY)
+    constexpr int GROUPS = 32 * CF / E;                                           // of E columns in a row: a lane stays with one
+    const int lane = threadIdx.x & 63, group = lane % GROUPS;
+    const f32x4* const from = reinterpret_cast<const f32x4*>(lds);
+#pragma unroll 4
+    for (int lr = lane / GROUPS; lr < ROWS; lr += 64 / GROUPS) {
+        const int row = row0 + lr;
+        f32x4 v[E / 4];
+#pragma unroll
+        for (int e = 0; e < E / 4; ++e) v[e] = from[lr * PIECES + ((E / 4 * group + e) ^ (lr & KEY))];
+        if (row < t.begin || row >= t.end || col >= N) continue;
+        mx_put<E, ALIGNED, ALIGNED>(ep, row, col, N, v, bias);
+    }
+}
 template <int RF, int CF, int IR, bool ALIGNED>
 __device__ __forceinline__ void mx_store(const f32x16 (&acc)[RF][CF], unsigned char* lds, const MxTile& t, int N, int m0, int n0w, const GemmEpilogue& ep) {
-    constexpr int PIECES = 8 * CF, KEY = (PIECES < 16 ? PIECES : 16) - 1;        // 16-byte pieces of a row; piece c of row r lies at c ^ (r & KEY)
-    constexpr int GROUPS = 4 * CF;                                                // of eight columns in a row: a lane stays with one
+    constexpr int PIECES = 8 * CF, KEY = (PIECES < 16 ? PIECES : 16) - 1;
     static_assert(RF % IR == 0, "whole rounds");
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-    const int group = lane % GROUPS, col = n0w + 8 * group;
+    const int col = n0w + (ep.y_f32 ? 4 * (lane % (8 * CF)) : 8 * (lane % (4 * CF)));
     const MxBias bias(ep, col, N);
     f32x4* const to = reinterpret_cast<f32x4*>(lds) + l32 * PIECES;
-    const f32x4* const from = reinterpret_cast<const f32x4*>(lds);
     for (int i0 = 0; i0 < RF; i0 += IR) {
 #pragma unroll
         for (int i = 0; i < RF; ++i) {
@@ -77,13 +91,8 @@ __device__ __forceinline__ void mx_store(const f32x16 (&acc)[RF][CF], unsigned c
                 at[(8 * j + 2 * half + 5) ^ (l32 & KEY)] = mx_part<3>(v);
             }
         }
-#pragma unroll 4
-        for (int lr = lane / GROUPS; lr < 32 * IR; lr += 64 / GROUPS) {
-            const int row = m0 + 32 * i0 + lr;
-            const f32x4 lo = from[lr * PIECES + ((2 * group) ^ (lr & KEY))], hi = from[lr * PIECES + ((2 * group + 1) ^ (lr & KEY))];
-            if (row < t.begin || row >= t.end || col >= N) continue;
-            mx_put8<ALIGNED>(ep, row, col, N, lo, hi, bias);
-        }
+        if (ep.y_f32) mx_store_rows<32 * IR, CF, 4, ALIGNED>(lds, t, N, m0 + 32 * i0, col, ep, bias);
+        else mx_store_rows<32 * IR, CF, 8, ALIGNED>(lds, t, N, m0 + 32 * i0, col, ep, bias);
     }
 }
 
@@ -121,8 +130,9 @@ __device__ __forceinline__ void mx_store_sums(float* sums, int splits, unsigned 
                 const int col = n0w + 32 * ((f0 + g) % CF) + 16 * b + 8 * half;
                 if (col >= N) continue;
                 const MxBias bias(ep, col, N);
-                if (ep.vec_ok) mx_put8<true>(ep, row, col, N, sum[4 * g + 2 * b], sum[4 * g + 2 * b + 1], bias);
-                else mx_put8<false>(ep, row, col, N, sum[4 * g + 2 * b], sum[4 * g + 2 * b + 1], bias);
+                const f32x4 v[2] = {sum[4 * g + 2 * b], sum[4 * g + 2 * b + 1]};
+                if (ep.vec_ok) mx_put<8, true, false>(ep, row, col, N, v, bias);
+                else mx_put<8, false, false>(ep, row, col, N, v, bias);
             }
         }
     }
