@@ -52,7 +52,7 @@ def linear(four=1, groups=-1, weights=1, given=0, m=4, n=64, k=256, act=0, out=0
     ("quantize 0 4 1048608 0 0 0", SHAPE, "2^20"), ("quantize 2 4 64 0 0 0", ARG, "dtype"), ("quantize 0 4 64 2 0 0", ARG, "layout"), ("quantize 0 4 64 0 1 0", ARG, "null"),
     ("quantize 0 4 64 1 2 0", ARG, "null"), ("quantize 1 4 64 1 3 0", ARG, "null"), ("quantize 0 4 64 0 0 8", ARG, "unaligned"),
     ("dequantize 3 4 64 0 0 0", ARG, "dtype"), ("dequantize 0 4 48 0 0 0", SHAPE, "cols"), ("dequantize 0 4 64 -1 0 0", ARG, "layout"), ("dequantize 0 4 64 0 3 0", ARG, "null"), ("dequantize 0 4 64 0 0 2", ARG, "unaligned"),
-    ("pack 64 40 0 0", SHAPE, "multiple of 32"), ("pack 0 64 0 0", SHAPE, "n=0"), ("pack 64 64 2 0", ARG, "null"), ("pack 64 64 0 4", ARG, "unaligned"),
+    ("pack 64 40 0 0", SHAPE, "multiple of 32"), ("pack 0 64 0 0", SHAPE, "n=0"), ("pack 16777217 64 0 0", SHAPE, "2^24"), ("pack 2147483647 64 0 0", SHAPE, "2^24"), ("pack 64 1048608 0 0", SHAPE, "2^20"), ("pack 64 64 2 0", ARG, "null"), ("pack 64 64 0 4", ARG, "unaligned"),
     (linear(k=48), SHAPE, "multiple of 32"), (linear(m=-1), ARG, "m=-1"), (linear(n=0), ARG, "n=0"), (linear(k=0), ARG, "k=0"), (linear(act=2), ARG, "act"), (linear(out=2), ARG, "out_dtype"),
     (linear(null=1), ARG, "null"), (linear(null=2), ARG, "null"), (linear(null=3), ARG, "null"), (linear(null=4), ARG, "null"), (linear(null=6), ARG, "null context"), (linear(off=8), ARG, "aligned"),
     (linear(k=1048608), SHAPE, "2^20"), (linear(m=16777217), SHAPE, "2^24"), (linear(n=16777217), SHAPE, "2^24"),
@@ -94,4 +94,5 @@ def test_tensor_sizes(rows, cols):
     assert rg.regione_mxfp4_scale_bytes(rows, cols, rg.MX_SCALE_STEPS) == mx.scale_steps(np.zeros((rows, blocks), np.uint8)).size
     n32, k256 = -(-rows // 32) * 32, -(-cols // 256) * 256
     assert rg.regione_packed_weight_mxfp4_bytes(rows, cols) == n32 * k256 // 2 + n32 * k256 // 32
+    assert rg.regione_packed_weight_mxfp4_bytes(2 ** 31 - 1, cols) == 2 ** 31 // 2 * k256 + 2 ** 31 // 32 * k256
     assert rg.regione_packed_weight_mxfp4_bytes(0, cols) == 0 and rg.regione_mxfp4_scale_bytes(0, cols, 1) == 0
