@@ -18,7 +18,7 @@ extern "C" {
  * has no such tile (some are bf16 or E4M3 only) or whose split does not fit the workspace. */
 int regione_tune_gemm(regione_ctx* ctx, int32_t wave_tile_blocks, int32_t k_splits);
 /* The same for regione_linear_mxfp4, regione_linear_grouped and regione_linear_mxfp4_grouped: tiles 1, 2, 4 and 8 are the
- * kernel of 16 rows with as many waves over K; 72, 62, 52, 42, 32, 51, 41, 31, 22, 21 and 11 are 10 * (rows / 32) + columns / 128.
+ * kernel of 16 rows and 32 columns per wave with as many waves over K, 9 the one of 16 columns and eight; 72, 62, 52, 42, 32, 51, 41, 31, 22, 21 and 11 are 10 * (rows / 32) + columns / 128.
  * Calls with groups take no K splits. */
 int regione_tune_mx(regione_ctx* ctx, int32_t tile, int32_t k_splits);
 

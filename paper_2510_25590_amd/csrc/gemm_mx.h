@@ -117,11 +117,13 @@ __device__ __forceinline__ void mx_put(const GemmEpilogue& ep, int row, int col,
         }
     } else {
         __bf16* y = static_cast<__bf16*>(ep.y) + at;
-        if constexpr (WIDE && E == 8) {
-            bf16x8 o;
+        if constexpr (WIDE) {
+            typedef __attribute__((ext_vector_type(E))) __bf16 Values;
+            typedef __attribute__((ext_vector_type(E / 2))) unsigned Piece;
+            Values o;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = static_cast<__bf16>(val[e]);
-            mx_put_piece<STREAM>(__builtin_bit_cast(u32x4, o), y);
+            for (int e = 0; e < E; ++e) o[e] = static_cast<__bf16>(val[e]);
+            mx_put_piece<STREAM>(__builtin_bit_cast(Piece, o), y);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) if (col + e < N) y[e] = static_cast<__bf16>(val[e]);
@@ -129,30 +131,32 @@ __device__ __forceinline__ void mx_put(const GemmEpilogue& ep, int row, int col,
     }
 }
 
-// Few rows: a wave owns 16 rows x 32 columns of a part of K and reads its operands straight from memory, the weights as they lie, with the loads of CHUNK steps in flight.  KW of a workgroup's
-// eight waves share K and meet in LDS, where the sums are formed in wave order; the others take further columns.  Such a launch is a chain of trips to memory and the reading of
-// the weights.
+// Few rows: a wave owns 16 rows x 16 * CF columns of a part of K and reads its operands straight from memory, the weights as they lie, with the loads of CHUNK steps in flight.  KW of a
+// workgroup's eight waves share K and meet in LDS, where the sums are formed in wave order; the others take further columns.  Such a launch is a chain of trips to memory and the reading of
+// the weights.  Where K is long and N short there are fewer workgroups than CUs, and registers for one trip only: 16 columns, eight steps at a time, two waves per SIMD; us, 32 columns and
+// two steps / so: one row x 3072 x 12288 9.3 / 7.2 (the weights at 6.4 TB/s and the launch), 16 rows x 3072 x 15360 13.7 / 9.5, but one row x 9216 x 3072 5.8 / 7.6, 96 rows x 2048 x 1024 of
+// 64 experts 15.8 / 46.6.
 constexpr int kMxSmallRows = 16, kMxSmallWaves = 8;
 
-template <int FMT, int KW>
-__global__ void __launch_bounds__(kMxSmallWaves * 64) __attribute__((amdgpu_waves_per_eu(4)))
+template <int FMT, int KW, int CF>
+__global__ void __launch_bounds__(kMxSmallWaves * 64) __attribute__((amdgpu_waves_per_eu(CF == 1 ? 2 : 4)))
 gemm_mx_small_kernel(MxOperands p, GemmEpilogue ep) {
-    constexpr int CF = 2, CHUNK = FMT == MX_FP4 ? 2 : 3, NW = kMxSmallWaves / KW;
+    constexpr int CHUNK = CF == 1 ? 8 : FMT == MX_FP4 ? 2 : 3, NW = kMxSmallWaves / KW, COLS = 16 * CF;
     __shared__ __attribute__((aligned(16))) f32x4 sums[KW == 1 ? 1 : kMxSmallWaves * CF * 64];
-    const int n_tiles = (p.n + 32 * NW - 1) / (32 * NW), unit = static_cast<int>(blockIdx.x) / n_tiles;
+    const int n_tiles = (p.n + COLS * NW - 1) / (COLS * NW), unit = static_cast<int>(blockIdx.x) / n_tiles;
     const MxTiles<kMxSmallRows> tiles(p);
     if (unit >= tiles.total) return;
     const MxTile t = tiles.find(p, unit);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kw = wave % KW;
     const int l16 = lane & 15, kc = lane >> 4;
-    const int n0 = ((static_cast<int>(blockIdx.x) - unit * n_tiles) * NW + wave / KW) * 32, n32 = (p.n + 31) & ~31;
+    const int n0 = ((static_cast<int>(blockIdx.x) - unit * n_tiles) * NW + wave / KW) * COLS, n32 = (p.n + 31) & ~31;
     const int per = (p.steps + KW - 1) / KW, s0 = kw * per, s1 = s0 + per < p.steps ? s0 + per : p.steps;
 
     const uint8_t* w = p.w + t.weight * p.w_stride;
     int nb = n0 >> 5;
     nb = nb < n32 / 32 ? nb : n32 / 32 - 1;                     // blocks past N repeat the last one; their sums are not stored
-    const int col0 = 8 * (l16 >> 2) + (l16 & 3);                // of the first fragment; the other one's is four further (see gemm_epilogue16)
+    const int col0 = CF == 1 ? (n0 & 16) + l16 : 8 * (l16 >> 2) + (l16 & 3);   // of the first fragment; the other one's is four further: a lane's results are 4 * CF consecutive columns
     const uint8_t* wp = w + ((static_cast<int64_t>(nb) * p.steps * 4 + (kc >> 1)) * 64 + (kc & 1) * 32 + col0) * 16;
     const uint8_t* wsp = w + static_cast<int64_t>(n32) * p.steps * 128 + (nb * 32 + col0) * 8 + 4 * (kc & 1);
     int row = t.row0 + l16;
@@ -206,11 +210,11 @@ gemm_mx_small_kernel(MxOperands p, GemmEpilogue ep) {
             for (int j = 0; j < CF; ++j) acc[j] += sums[((wave + v) * CF + j) * 64 + lane];
     }
     if (ep.bias) ep.bias += static_cast<int64_t>(t.weight) * p.n;
-    const int col = n0 + 8 * kc;
+    const int col = n0 + 4 * CF * kc;
     if (t.row0 + l16 >= t.end || t.row0 + l16 < t.begin || col >= p.n) return;
     const MxBias bias(ep, col, p.n);
-    if (ep.vec_ok) mx_put<8, true, false>(ep, row, col, p.n, acc, bias);
-    else mx_put<8, false, false>(ep, row, col, p.n, acc, bias);
+    if (ep.vec_ok) mx_put<4 * CF, true, false>(ep, row, col, p.n, acc, bias);
+    else mx_put<4 * CF, false, false>(ep, row, col, p.n, acc, bias);
 }
 
 }  // namespace

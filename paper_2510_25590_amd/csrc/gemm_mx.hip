@@ -4,41 +4,48 @@
 
 namespace {
 
-template <int FMT, int KW>
+template <int FMT, int KW, int CF>
 int launch_small(regione_ctx* ctx, const MxOperands& p, const GemmEpilogue& ep) {
-    constexpr int COLS = 32 * kMxSmallWaves / KW;
+    constexpr int COLS = 16 * CF * kMxSmallWaves / KW;
     const int64_t tiles = mx_most_row_tiles(p, kMxSmallRows) * ((p.n + COLS - 1) / COLS);
     if (tiles >= (int64_t{1} << 32) / (kMxSmallWaves * 64)) RG_FAIL(REGIONE_ERR_UNSUPPORTED, "linear: a result of %d x %d", p.m, p.n);
-    hipLaunchKernelGGL((gemm_mx_small_kernel<FMT, KW>), dim3(static_cast<unsigned>(tiles)), dim3(kMxSmallWaves * 64), 0, ctx->stream, p, ep);
+    hipLaunchKernelGGL((gemm_mx_small_kernel<FMT, KW, CF>), dim3(static_cast<unsigned>(tiles)), dim3(kMxSmallWaves * 64), 0, ctx->stream, p, ep);
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }
 template <int FMT>
-int launch_small(regione_ctx* ctx, int waves, const MxOperands& p, const GemmEpilogue& ep) {
-    return waves == 1 ? launch_small<FMT, 1>(ctx, p, ep) : waves == 2 ? launch_small<FMT, 2>(ctx, p, ep) : waves == 4 ? launch_small<FMT, 4>(ctx, p, ep) : launch_small<FMT, 8>(ctx, p, ep);
+int launch_small(regione_ctx* ctx, int code, const MxOperands& p, const GemmEpilogue& ep) {
+    switch (code) {
+        case 1: return launch_small<FMT, 1, 2>(ctx, p, ep);
+        case 2: return launch_small<FMT, 2, 2>(ctx, p, ep);
+        case 4: return launch_small<FMT, 4, 2>(ctx, p, ep);
+        case 8: return launch_small<FMT, 8, 2>(ctx, p, ep);
+    }
+    return launch_small<FMT, 8, 1>(ctx, p, ep);
 }
 
 // ---- which kernel a product gets
 //
 // A plan's time is estimated as a start, whole and partial loads of the chip by workgroups (a fixed part and a part per step of K, which grow with the workgroups that share a CU, and the
-// activation, which they do one after the other), not less than the weights take from HBM, and the results' way out; a K split adds its sums' way out and back, the kernel of 16 rows what
-// its repeated reading of the weights takes.  The host does not know the groups' sizes: they are taken as random (exponentially distributed), a group of mean length s then has
-// 1 / (1 - exp(-R / s)) tiles of R rows.  All constants are fitted to every tile, K split and number of waves of 1193 products in 4 bits and 803 in bf16 (1-16384 rows, 64-12288 columns,
-// K 256-15360, up to 64 groups, equal and random, with and without activation): over 597 / 402 others the choice is 2.0 / 4.7 % behind the best plan measured on average, 10 / 23 % in the
-// twentieth of them where it is furthest, 54 / 58 % at most (groups whose sizes are far from the assumed ones).
+// activation, which they do one after the other), what the weights take from HBM (the root of both squares: the longer of them, and a little for the other), and the results' way out; a K split
+// adds its sums' way out and back, the kernel of 16 rows what its repeated reading of the weights takes.  The host does not know the groups' sizes: they are taken as random (exponentially distributed), a group of mean length s then has
+// 1 / (1 - exp(-R / s)) tiles of R rows.  All constants are fitted to every tile, K split and number of waves of 1978 products in 4 bits and 1312 in bf16 (1-16384 rows, 64-14400 columns,
+// K 256-16000, up to 64 groups, equal and random, with and without activation): over 990 / 657 others the choice is 1.9 / 2.3 % behind the best plan measured on average, 9 / 11 % in the
+// twentieth of them where it is furthest, 35 % at most (groups whose sizes are far from the assumed ones).
 // us, another tile / the choice: 820 x 12288 x 3072 256 x 256 32.0 / 192 x 256 25.8; 820 x 3072 x 12288 256 x 256 61.7 / 128 x 128 27.4; 128 x 3072 x 12288 unsplit 19.8 / four K splits
 // 13.7; 8704 x 12288 x 3072 128 x 128 204 / 128 x 256 172; one row x 9216 x 3072 all waves over columns 9.8 / four over K 5.2.
-struct MxPlan { int tile, splits; };      // tile 1, 2, 4, 8: the kernel of 16 rows with as many waves over K
+// Left out, a kernel would cost the products that it is best for: the one of 16 rows with one, two, four and eight waves over K 32, 7, 18 and 48 %, with 16 columns 49 %.
+struct MxPlan { int tile, splits; };      // tile 1, 2, 4, 8: the kernel of 16 rows and 32 columns per wave with as many waves over K; 9: with eight, 16 columns
 struct MxTileCost { int code, per_cu; double fixed, step, more; };               // us, us per step, and what each further workgroup of a CU adds to the latter (as a share)
-struct MxSmallCost { int waves; double fixed, step, work; };                      // us, us per step of a wave, us per 1e5 steps of columns
-struct MxCosts { MxTileCost tile[11]; MxSmallCost small[4]; double start, hbm, out, gelu; };     // us, bytes of weights per us, results per us, us per 100 kB of a tile's sums
+struct MxSmallCost { int code; double fixed, step, work; };                       // us and us per step of a wave, per load of the chip; us per 1e5 steps of columns
+struct MxCosts { MxTileCost tile[11]; MxSmallCost small[5]; double start, hbm, out, gelu; };     // us, bytes of weights per us, results per us, us per 100 kB of a tile's sums
 constexpr MxCosts kMxCosts[2] = {
-    {{{72, 1, 2.68, 0.937, 0.0}, {62, 1, 2.27, 0.805, 0.0}, {52, 1, 1.79, 0.678, 0.0}, {42, 2, 0.83, 0.563, 0.951}, {32, 2, 0.41, 0.483, 0.926}, {51, 2, 0.83, 0.393, 1.088},
-      {41, 2, 0.39, 0.328, 1.131}, {31, 3, 0.12, 0.268, 1.119}, {22, 2, 0.03, 0.378, 1.045}, {21, 3, 0.00, 0.216, 1.179}, {11, 3, 0.24, 0.165, 1.368}},
-     {{1, 0.49, 0.198, 1.14}, {2, 0.00, 0.281, 1.16}, {4, 0.22, 0.206, 1.23}, {8, 0.60, 0.028, 1.32}}, 3.61, 7.73e6, 0.98e6, 0.69},
-    {{{72, 1, 2.90, 1.178, 0.0}, {62, 1, 2.22, 1.004, 0.0}, {52, 1, 2.21, 0.855, 0.0}, {42, 2, 1.18, 0.651, 1.009}, {32, 2, 0.83, 0.543, 1.056}, {51, 2, 0.93, 0.453, 1.459},
-      {41, 2, 0.67, 0.363, 1.636}, {31, 3, 0.44, 0.299, 1.380}, {22, 2, 0.60, 0.405, 1.275}, {21, 3, 0.29, 0.228, 1.463}, {11, 3, 0.51, 0.177, 1.695}},
-     {{1, 0.00, 0.408, 1.23}, {2, 0.01, 0.451, 1.07}, {4, 0.11, 0.428, 1.04}, {8, 0.25, 0.344, 1.15}}, 3.69, 6.63e6, 1.49e6, 0.78}};
+    {{{72, 1, 2.82, 0.922, 0.000}, {62, 1, 2.37, 0.799, 0.000}, {52, 1, 2.46, 0.597, 0.000}, {42, 2, 1.36, 0.505, 1.118}, {32, 2, 0.90, 0.434, 1.148}, {51, 2, 0.98, 0.384, 1.119},
+      {41, 2, 0.82, 0.295, 1.348}, {31, 3, 0.57, 0.243, 1.305}, {22, 2, 0.47, 0.344, 1.268}, {21, 3, 0.30, 0.202, 1.312}, {11, 3, 0.45, 0.164, 1.420}},
+     {{1, 0.06, 0.317, 0.83}, {2, 0.23, 0.317, 0.74}, {4, 0.43, 0.282, 0.74}, {8, 0.70, 0.222, 0.71}, {9, 0.72, 0.186, 0.37}}, 3.47, 11.55e6, 1.00e6, 0.70},
+    {{{72, 1, 2.94, 1.199, 0.000}, {62, 1, 2.28, 1.017, 0.000}, {52, 1, 2.32, 0.802, 0.000}, {42, 2, 1.30, 0.622, 1.153}, {32, 2, 1.00, 0.520, 1.200}, {51, 2, 1.02, 0.458, 1.404},
+      {41, 2, 0.83, 0.342, 1.728}, {31, 3, 0.69, 0.283, 1.504}, {22, 2, 0.75, 0.394, 1.376}, {21, 3, 0.54, 0.214, 1.592}, {11, 3, 0.76, 0.174, 1.682}},
+     {{1, 0.00, 0.499, 0.79}, {2, 0.25, 0.480, 0.77}, {4, 0.45, 0.421, 0.72}, {8, 0.61, 0.325, 0.83}, {9, 1.01, 0.096, 0.72}}, 3.59, 10.78e6, 1.52e6, 0.65}};
 
 double row_tiles_expected(const MxOperands& p, int R) {
     const double most = static_cast<double>(mx_most_row_tiles(p, R)), g = p.n_groups < p.m ? p.n_groups : p.m;
@@ -69,18 +76,17 @@ MxPlan choose(int fmt, const MxOperands& p, int act, size_t part_bytes) {
             const double loads = floor(units * s / (256.0 * t.per_cu)), rest = units * s - loads * 256.0 * t.per_cu;
             auto load = [&](double shared) { return t.fixed + per * t.step * (1.0 + t.more * (shared - 1.0)) + gelu * shared; };
             double us = loads * load(t.per_cu) + (rest > 0.0 ? load(ceil(rest / 256.0)) : 0.0);
-            if (us < weights) us = weights;
-            us += static_cast<double>(p.m) * p.n / c.out;
-            if (s > 1) us += 0.97 + 0.295 * units * s * tile_kb / 1e3 + 0.0196 * s * tile_kb;
+            us = sqrt(us * us + weights * weights) + static_cast<double>(p.m) * p.n / c.out;
+            if (s > 1) us += 0.91 + 0.288 * units * s * tile_kb / 1e3 + 0.0187 * s * tile_kb;
             consider(t.code, s, c.start + us);
         }
     }
     if (p.m > 48 * static_cast<int64_t>(groups)) return best;     // (more than what the kernel of 16 rows was fitted to)
     for (const MxSmallCost& t : c.small) {
-        const int C = 256 / t.waves;
+        const int waves = t.code == 9 ? 8 : t.code, C = t.code == 9 ? 16 : 32 * kMxSmallWaves / waves, slots = t.code == 9 ? 256 : 512;
         const double units = row_tiles_expected(p, kMxSmallRows) * ((p.n + C - 1) / C);
-        const double us = t.fixed + t.step * ((p.steps + t.waves - 1) / t.waves) + t.work * 1e-5 * units * p.steps * C;
-        consider(t.waves, 1, c.start + (us < weights ? weights : us));
+        const double us = ceil(units / slots) * (t.fixed + t.step * ((p.steps + waves - 1) / waves)) + t.work * 1e-5 * units * p.steps * C;
+        consider(t.code, 1, c.start + sqrt(us * us + weights * weights));
     }
     return best;
 }
@@ -100,7 +106,7 @@ int launch(regione_ctx* ctx, int fmt, const MxOperands& p, const GemmEpilogue& e
     ProfScope prof(ctx, REGIONE_PROF_GEMM);
     MxPlan to = plan(ctx, fmt, p, ep.act);
     if (ctx->mx_force_tile) to = {ctx->mx_force_tile, ctx->mx_force_splits > 0 && !p.offsets ? ctx->mx_force_splits : 1};
-    if (to.tile <= 8) return fmt == MX_FP4 ? launch_small<MX_FP4>(ctx, to.tile, p, ep) : launch_small<MX_BF16>(ctx, to.tile, p, ep);
+    if (to.tile < 10) return fmt == MX_FP4 ? launch_small<MX_FP4>(ctx, to.tile, p, ep) : launch_small<MX_BF16>(ctx, to.tile, p, ep);
     return fmt == MX_FP4 ? rg_mx_tile_4bit(ctx, to.tile, p, to.splits, ep) : rg_mx_tile_bf16(ctx, to.tile, p, to.splits, ep);
 }
 
@@ -152,7 +158,7 @@ extern "C" int regione_linear_grouped(regione_ctx* ctx, const void* x, const voi
 extern "C" int regione_tune_mx(regione_ctx* ctx, int32_t tile, int32_t k_splits) {
     if (!ctx) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: null context");
     bool known = tile == 0;
-    for (int t : {1, 2, 4, 8, 72, 62, 52, 42, 32, 51, 41, 31, 22, 21, 11}) known = known || t == tile;
+    for (int t : {1, 2, 4, 8, 9, 72, 62, 52, 42, 32, 51, 41, 31, 22, 21, 11}) known = known || t == tile;
     if (!known || k_splits < 0 || k_splits > 16) RG_FAIL(REGIONE_ERR_INVALID_ARG, "tune_mx: no tile %d, or k_splits=%d is not in 0..16", tile, k_splits);
     ctx->mx_force_tile = tile;
     ctx->mx_force_splits = k_splits;

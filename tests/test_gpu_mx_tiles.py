@@ -8,7 +8,7 @@ from paper_2510_25590_amd import binding as rg
 
 pytestmark = pytest.mark.gpu
 
-TILES = [1, 2, 4, 8, 72, 62, 52, 42, 32, 51, 41, 31, 22, 21, 11]
+TILES = [1, 2, 4, 8, 9, 72, 62, 52, 42, 32, 51, 41, 31, 22, 21, 11]
 
 
 @pytest.fixture
@@ -75,7 +75,7 @@ def test_tiles_of_groups(ctx, tile, fmt, sizes, first, m, n, k, use):
     assert np.array_equal(y.cpu().double().numpy(), want)
 
 
-@pytest.mark.parametrize("tile", [t for t in TILES if t > 8])
+@pytest.mark.parametrize("tile", [t for t in TILES if t > 9])
 @pytest.mark.parametrize("act,out,offset", [(False, torch.bfloat16, 0), (True, torch.bfloat16, 0), (True, torch.float32, 0), (True, torch.bfloat16, 3), (True, torch.float32, 1)])
 @pytest.mark.parametrize("n", [264, 261])
 def test_k_splits_with_bias_and_activation(ctx, tile, act, out, offset, n):
