@@ -150,7 +150,7 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
     const int local = static_cast<int>(blockIdx.x >> 3), unit = static_cast<int>(blockIdx.x & 7) * per_xcd + local;     // each XCD a contiguous range (see pp_unit)
     if (local >= per_xcd || unit >= units) return;
     int m_tile, n_tile, split = 0;
-    if (splits == 1) {
+    if (FMT == MX_BF16 || splits == 1) {               // (bf16 comes in groups, which have no K splits)
         tile_coords(unit, m_tiles, n_tiles, m_tiles > 8 ? 4 : m_tiles, m_tile, n_tile);
     } else {
         m_tile = unit % m_tiles;
@@ -324,7 +324,7 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
 
     const int m0 = t.row0, n0w = n0 + wave * (CF * 32);
     if (ep.bias) ep.bias += static_cast<int64_t>(t.weight) * p.n;
-    if (splits > 1) {
+    if (FMT == MX_FP4 && splits > 1) {
         // As in pp_finish: every split leaves its sums in register order and the workgroup that arrives last adds all of them in split order.
         const int tile = n_tile * m_tiles + m_tile;
         float* mine = partial + (static_cast<int64_t>(tile) * splits + split) * T::PART_FLOATS;
