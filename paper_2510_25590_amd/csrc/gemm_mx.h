@@ -4,7 +4,7 @@
 //
 // Both formats move the same bytes: a K-step is 128 bytes of every row, 64 bf16 or 256 E2M1 values, and a lane feeds 16 of them to a matrix instruction
 // (16x16 or 32x32 results), in 4 bits together with the byte of their scale: the instruction's lane holds 32 values of one row, which is one block.  The instruction multiplies E2M1 values exactly and applies both powers of two; sums are float32.  The weights are the first operand, so that a
-// lane ends up with eight consecutive columns of a row and the other products' epilogue serves here, too.
+// lane ends up with consecutive columns of a row.
 #pragma once
 #include "gemm_pp.h"
 #include "mx.h"

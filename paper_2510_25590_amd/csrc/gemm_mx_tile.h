@@ -30,6 +30,7 @@ template <int FMT, int RF, int CF> struct MxTileShape {
     static_assert(ROW_SCALES + CF <= 4, "a wave per piece");
     static constexpr int STORE_ROWS = RF % 2 == 0 ? 2 : 1;                         // rows of fragments per wave that mx_store leaves in LDS at a time
     static constexpr unsigned STORE = STORE_ROWS * CF * 4096u, LDS_BYTES = S_BASE + 2 * SCALES > 4 * STORE ? S_BASE + 2 * SCALES : 4 * STORE;
+    static_assert(LDS_BYTES <= 65536u, "more has to be granted");
     static constexpr int64_t PART_FLOATS = static_cast<int64_t>(ROWS) * COLS;
 };
 
@@ -364,10 +365,6 @@ int launch_mx_tile(regione_ctx* ctx, const MxOperands& p, int splits, const Gemm
         RG_FAIL(REGIONE_ERR_WORKSPACE, "linear: %d K-splits of a %d x %d result exceed the workspace", used, p.m, p.n);
     const int64_t workgroups = (row_tiles * n_tiles * used + 7) / 8 * 8;
     if (workgroups >= (int64_t{1} << 32) / T::THREADS) RG_FAIL(REGIONE_ERR_UNSUPPORTED, "linear: a result of %d x %d", p.m, p.n);
-    if (T::LDS_BYTES > 65536u) {
-        static std::atomic<uint64_t> granted{0};
-        if (int rc = rg_grant_lds(ctx, reinterpret_cast<const void*>(gemm_mx_tile_kernel<FMT, RF, CF, LOOK, WAVES>), granted, T::LDS_BYTES)) return rc;
-    }
     hipLaunchKernelGGL((gemm_mx_tile_kernel<FMT, RF, CF, LOOK, WAVES>), dim3(static_cast<unsigned>(workgroups)), dim3(T::THREADS), T::LDS_BYTES, ctx->stream, p, used, per, ctx->gemm_part, ctx->gemm_arrived, ep);
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
