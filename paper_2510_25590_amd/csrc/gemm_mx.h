@@ -85,11 +85,12 @@ __device__ __forceinline__ float mx_gelu(float x) {
 }
 // The end of E consecutive columns of a row, those below N.  WIDE: all of them are, and 16-byte pieces are aligned.  STREAM: past the caches, where stores cover whole pieces of a row side by
 // side: 16384 x 4096 x 2048 120 -> 114 us, 8704 x 9216 x 3072 148 -> 143; with a quantiser reading the result behind it 128.2 -> 126.7 and, 205 x 12288 x 3072, 18.1 -> 17.1.
-struct MxBias {
+struct MxBias {                // of eight columns; those past N, and all without a bias, are zero by the resource's size: no branches, all loads in flight together
     float v[8];
     __device__ __forceinline__ MxBias(const GemmEpilogue& ep, int col, int N) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(ep.bias), 0, ep.bias ? N * 4 : 0, 0x00027000);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = ep.bias && col + e < N ? ep.bias[col + e] : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rsrc, (col + e) * 4, 0, 0));
     }
 };
 template <bool STREAM, typename P> __device__ __forceinline__ void mx_put_piece(const P& v, void* to) {

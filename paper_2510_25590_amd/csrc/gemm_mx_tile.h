@@ -203,14 +203,6 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
                        wave < T::ROW_SCALES + CF && s_left > 0 ? static_cast<int>(s_left * 8) : 0};
     const unsigned as_get = T::S_BASE + l32 * 8u + half * 4u, ws_get = T::S_BASE + T::ROW_SCALES * 1024u + (wave * (CF * 32) + feature) * 8u + half * 4u;
 
-    f32x16 acc[RF][CF];
-#pragma unroll
-    for (int i = 0; i < RF; ++i)
-#pragma unroll
-        for (int j = 0; j < CF; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
     auto each = [&](auto from, auto to, auto f, auto self) __attribute__((always_inline)) {
         if constexpr (decltype(from)::value < decltype(to)::value) {
             f(from);
@@ -277,6 +269,14 @@ gemm_mx_tile_kernel(MxOperands p, int splits, int steps_per_split, float* __rest
         load_scales(b);
         each(zero{}, phases{}, [&](auto q) __attribute__((always_inline)) { each(zero{}, columns{}, [&](auto j) __attribute__((always_inline)) { load_w(b, q, j); __builtin_amdgcn_sched_barrier(0); }, each); }, each);
     }, each);
+    f32x16 acc[RF][CF];                                                            // (while the loads are on their way)
+#pragma unroll
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int j = 0; j < CF; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
     each(zero{}, rows{}, [&](auto i) __attribute__((always_inline)) { write_a(0, std::integral_constant<int, -1>{}, i); }, each);
     if constexpr (FMT == MX_FP4) *reinterpret_cast<u32x4*>(lds_raw + T::S_BASE + wave * 1024u + lane * 16u) = first_scales;
     mx_lds_done();
