@@ -96,3 +96,23 @@ def test_tensor_sizes(rows, cols):
     assert rg.regione_packed_weight_mxfp4_bytes(rows, cols) == n32 * k256 // 2 + n32 * k256 // 32
     assert rg.regione_packed_weight_mxfp4_bytes(2 ** 31 - 1, cols) == 2 ** 31 // 2 * k256 + 2 ** 31 // 32 * k256
     assert rg.regione_packed_weight_mxfp4_bytes(0, cols) == 0 and rg.regione_mxfp4_scale_bytes(0, cols, 1) == 0
+
+
+def test_every_choice_covers_its_result(run):
+    """Whatever kernel a call gets, its grid has a workgroup for every tile that the result, or the worst sizes of its groups, can have; and every kernel is chosen for some call."""
+    import itertools
+    shapes = list(itertools.product((1, 4, 16, 40, 64, 130, 205, 300, 410, 820, 1382, 2048, 8704), (64, 768, 1000, 3072, 7568, 9216, 12288), (64, 128, 256, 1024, 3072, 12288, 15360)))
+    calls = [(four, groups, m, n, k) for m, n, k in shapes for four, groups in ((1, -1), (1, 2), (1, 16), (1, 64), (0, 1), (0, 4), (0, 16), (0, 64))]
+    answers = run([BF] + [linear(four=f, groups=g, weights=max(g, 1), m=m, n=n, k=k) for f, g, m, n, k in calls])[1:]
+    seen = set()
+    for (four, groups, m, n, k), (code, launches, message) in zip(calls, answers):
+        assert code == rg.OK and len(launches) == 1, message
+        (x, _, _), lds, kernel = launches[0]
+        kind, numbers = re.search(r"gemm_mx_(small|tile)_kernel<([\d, ]+)>", kernel).groups()
+        args = tuple(int(v) for v in numbers.split(", "))
+        seen.add((kind,) + args)
+        assert args[0] == four
+        rows, cols = (16, 16 * args[2] * 8 // args[1]) if kind == "small" else (32 * args[1], 128 * args[2])
+        tiles = -(-m // rows) if groups == -1 else m // rows + min(groups, m)
+        assert x >= tiles * -(-n // cols) and lds <= 65536, (kernel, m, n, k, groups)
+    assert len({s for s in seen if s[1] == 1}) == len({s for s in seen if s[1] == 0}) == 16, sorted(seen)
