@@ -7,6 +7,7 @@ fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -230,6 +231,26 @@ class Context:
             pass
 
 
+@contextlib.contextmanager
+def _on_stream_of(ctx, *inputs):
+    """For the calls that make tensors themselves: what is allocated inside belongs to the context's stream, where the library works on it, so that the allocator hands its memory on only
+    behind that work.  A caller on another stream: the context's stream first waits for the caller's, which made `inputs`, and the caller's afterwards for the context's; torch keeps the
+    memory of `inputs`, and that of the results (to be appended to the list that is yielded), until both streams are done with it."""
+    import torch
+    caller, results = torch.cuda.current_stream(ctx.stream.device), []
+    if caller == ctx.stream:
+        yield results
+        return
+    ctx.stream.wait_stream(caller)
+    for t in inputs:
+        t.record_stream(ctx.stream)
+    with torch.cuda.stream(ctx.stream):
+        yield results
+    caller.wait_stream(ctx.stream)
+    for t in results:
+        t.record_stream(caller)
+
+
 def make_stream_weights(tensors: dict) -> StreamWeights:
     """dict name -> torch CUDA tensor (missing names become NULL).  The caller keeps the tensors alive."""
     w = StreamWeights()
@@ -295,13 +316,15 @@ def make_stream_weights_fp8(ctx, tensors: dict):
     for name in ("w_qkv", "w_o", "w_1", "w_2"):
         if name not in tensors:          # a single-stream block has w_1 and w_2 only
             continue
-        w = tensors[name].contiguous()
+        w = tensors[name]
         n, k = w.shape
-        codes = torch.empty((n, k), dtype=torch.uint8, device=w.device)
-        scale = torch.empty(n, dtype=torch.float32, device=w.device)
-        regione_quantize_rows_fp8(ctx, w, n, k, codes, scale)
-        packed = torch.zeros(regione_packed_weight_elems(n, k), dtype=torch.uint8, device=w.device)
-        regione_pack_weight_fp8(ctx, codes, n, k, packed)
+        with _on_stream_of(ctx, w) as results:
+            codes = torch.empty((n, k), dtype=torch.uint8, device=w.device)
+            scale = torch.empty(n, dtype=torch.float32, device=w.device)
+            regione_quantize_rows_fp8(ctx, w.contiguous(), n, k, codes, scale)
+            packed = torch.zeros(regione_packed_weight_elems(n, k), dtype=torch.uint8, device=w.device)
+            regione_pack_weight_fp8(ctx, codes, n, k, packed)
+            results += packed, scale, codes
         keep[name] = (packed, scale, codes)
         setattr(w8, name, packed.data_ptr())
         setattr(w8, "s_" + name[2:], scale.data_ptr())
@@ -556,9 +579,11 @@ def quantize_rows_mxfp4(ctx, x, layout: int = MX_SCALE_STEPS):
     """Convenience: (codes, scale bytes) of a CUDA tensor [rows, cols], bf16 or float32, as new tensors."""
     import torch
     rows, cols = x.shape
-    q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device)
-    scale = torch.empty(regione_mxfp4_scale_bytes(rows, cols, layout), dtype=torch.uint8, device=x.device)
-    regione_quantize_rows_mxfp4(ctx, x.contiguous(), FP32 if x.dtype == torch.float32 else BF16, rows, cols, layout, q, scale)
+    with _on_stream_of(ctx, x) as results:
+        q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device)
+        scale = torch.empty(regione_mxfp4_scale_bytes(rows, cols, layout), dtype=torch.uint8, device=x.device)
+        regione_quantize_rows_mxfp4(ctx, x.contiguous(), FP32 if x.dtype == torch.float32 else BF16, rows, cols, layout, q, scale)
+        results += q, scale
     return q, scale
 
 
@@ -566,9 +591,11 @@ def pack_weight_mxfp4(ctx, w):
     """Convenience: quantises a row-major CUDA tensor [n, k], bf16 or float32, and packs it into a new tensor in the library's layout."""
     import torch
     n, k = w.shape
-    q, scale = quantize_rows_mxfp4(ctx, w, MX_SCALE_ROWS)
-    out = torch.empty(regione_packed_weight_mxfp4_bytes(n, k), dtype=torch.uint8, device=w.device)
-    regione_pack_weight_mxfp4(ctx, q, scale, n, k, out)
+    with _on_stream_of(ctx, w) as results:
+        q, scale = quantize_rows_mxfp4(ctx, w, MX_SCALE_ROWS)
+        out = torch.empty(regione_packed_weight_mxfp4_bytes(n, k), dtype=torch.uint8, device=w.device)
+        regione_pack_weight_mxfp4(ctx, q, scale, n, k, out)
+        results.append(out)
     return out
 
 
@@ -625,6 +652,8 @@ def pack_weight(ctx, w):
     import torch
     n, k = w.shape
     assert w.dtype == ctx.torch_dtype, (w.dtype, ctx.torch_dtype)
-    out = torch.empty(regione_packed_weight_elems(n, k), dtype=w.dtype, device=w.device)
-    regione_pack_weight(ctx, w.contiguous(), n, k, out)
+    with _on_stream_of(ctx, w) as results:
+        out = torch.empty(regione_packed_weight_elems(n, k), dtype=w.dtype, device=w.device)
+        regione_pack_weight(ctx, w.contiguous(), n, k, out)
+        results.append(out)
     return out
