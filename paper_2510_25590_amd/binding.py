@@ -575,9 +575,17 @@ def regione_tune_mx(ctx, tile: int, k_splits: int = 0):
     _check(lib().regione_tune_mx(ctx.handle, tile, k_splits))
 
 
+def _check_rows(ctx, who, x):
+    """Before the memory of anything else is read as bf16 or float32 rows."""
+    import torch
+    if x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32) or x.device != ctx.stream.device:
+        raise RegionEError(ERR_INVALID_ARG, f"{who}: {x.dtype} {tuple(x.shape)} on {x.device}, not bf16 or float32 [rows, cols] on {ctx.stream.device}")
+
+
 def quantize_rows_mxfp4(ctx, x, layout: int = MX_SCALE_STEPS):
     """Convenience: (codes, scale bytes) of a CUDA tensor [rows, cols], bf16 or float32, as new tensors."""
     import torch
+    _check_rows(ctx, "quantize_rows_mxfp4", x)
     rows, cols = x.shape
     with _on_stream_of(ctx, x) as results:
         q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device)
@@ -590,6 +598,7 @@ def quantize_rows_mxfp4(ctx, x, layout: int = MX_SCALE_STEPS):
 def pack_weight_mxfp4(ctx, w):
     """Convenience: quantises a row-major CUDA tensor [n, k], bf16 or float32, and packs it into a new tensor in the library's layout."""
     import torch
+    _check_rows(ctx, "pack_weight_mxfp4", w)
     n, k = w.shape
     with _on_stream_of(ctx, w) as results:
         q, scale = quantize_rows_mxfp4(ctx, w, MX_SCALE_ROWS)
