@@ -19,7 +19,7 @@ extern "C" {
 int regione_tune_gemm(regione_ctx* ctx, int32_t wave_tile_blocks, int32_t k_splits);
 /* The same for regione_linear_mxfp4, regione_linear_grouped and regione_linear_mxfp4_grouped: tiles 1, 2, 4 and 8 are the
  * kernel of 16 rows and 32 columns per wave with as many waves over K, 9 the one of 16 columns and eight; 72, 62, 52, 42, 32, 51, 41, 31, 22, 21 and 11 are 10 * (rows / 32) + columns / 128.
- * Calls with groups take no K splits. */
+ * The kernels of 16 rows and calls with groups take no K splits: they stay as they are. */
 int regione_tune_mx(regione_ctx* ctx, int32_t tile, int32_t k_splits);
 
 /* The tile and the number of K splits that a product of m rows, n columns and k elements gets by itself, with a K-split workspace

@@ -105,7 +105,8 @@ MxPlan plan(regione_ctx* ctx, int fmt, const MxOperands& p, int act) {
 int launch(regione_ctx* ctx, int fmt, const MxOperands& p, const GemmEpilogue& ep) {
     ProfScope prof(ctx, REGIONE_PROF_GEMM);
     MxPlan to = plan(ctx, fmt, p, ep.act);
-    if (ctx->mx_force_tile) to = {ctx->mx_force_tile, ctx->mx_force_splits > 0 && !p.offsets ? ctx->mx_force_splits : 1};
+    if (ctx->mx_force_tile) to = {ctx->mx_force_tile, 1};
+    if (ctx->mx_force_splits > 0 && !p.offsets) to.splits = ctx->mx_force_splits;
     if (to.tile < 10) return fmt == MX_FP4 ? launch_small<MX_FP4>(ctx, to.tile, p, ep) : launch_small<MX_BF16>(ctx, to.tile, p, ep);
     return fmt == MX_FP4 ? rg_mx_tile_4bit(ctx, to.tile, p, to.splits, ep) : rg_mx_tile_bf16(ctx, to.tile, p, to.splits, ep);
 }
