@@ -264,8 +264,8 @@ int regione_linear_fp8(regione_ctx* ctx, const void* xq, const float* x_scale, c
  *   features x 64 inputs (lane l of 64: feature l % 32, the 16 bytes of inputs 32 * (l / 32) on), blocks ordered feature
  *   block major; behind them the scales of the features (rounded up to 32) in steps.
  * regione_linear_mxfp4: y[m, n] = act(sum over blocks of 2^(e_x + e_w) sum_i xq wq + b[n]): products exact, sums in
- *   float32.  xq uint8 [m, k / 2], x_scale in steps; y of out_dtype.  n at most 2^24, k at most 2^20.  A block of scale 255 makes its row (of a weight:
- *   its column) NaN. */
+ *   float32.  xq uint8 [m, k / 2], x_scale in steps; y of out_dtype.  m and n at most 2^24, k at most 2^20 (as is cols
+ *   above, of at most 2^31 - 1 rows).  A block of scale 255 makes its row (of a weight: its column) NaN. */
 enum { REGIONE_MX_SCALE_ROWS = 0, REGIONE_MX_SCALE_STEPS = 1 };
 int64_t regione_mxfp4_scale_bytes(int64_t rows, int32_t cols, int32_t scale_layout);
 int regione_quantize_rows_mxfp4(regione_ctx* ctx, const void* x, int32_t x_dtype, int64_t rows, int32_t cols, int32_t scale_layout,
@@ -284,7 +284,9 @@ int regione_linear_mxfp4(regione_ctx* ctx, const void* xq, const void* x_scale, 
  *   w_packed: n_weights packed weights [n, k] one after the other; b_opt [n_weights, n] float32 or NULL.
  * The host knows neither the groups' sizes nor the number of rows that belong to one; rows of x that belong to no
  * group do not matter, and such rows of y stay as they were.  Offsets outside [0, m] are taken as the nearer end, a group that ends before it
- * starts is empty, and a group whose weight is not in [0, n_weights) is left out.  At most 65536 groups.
+ * starts is empty, and a group whose weight is not in [0, n_weights) is left out.  No two groups may share a row: if
+ * they do, parts of that row come out as any of theirs, and rows of any group may stay as they were.  At most 65536
+ * groups, m at most 2^24, n and k as for regione_linear_mxfp4.
  *   regione_linear_grouped: x bf16 [m, k], k a multiple of 64, weights of regione_pack_weight. */
 int regione_linear_grouped(regione_ctx* ctx, const void* x, const void* w_packed, const float* b_opt, const int32_t* group_offsets,
                            const int32_t* group_weight_opt, int32_t n_groups, int32_t n_weights, int32_t m, int32_t n, int32_t k,

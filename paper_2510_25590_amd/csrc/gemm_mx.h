@@ -40,7 +40,8 @@ __device__ __forceinline__ int mx_prefix(int v) {              // sum over the l
     v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);     // the first row's last lane to the second row, the third's to the fourth
     return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // the second row's last lane to both above
 }
-// Row tiles of a launch: of all rows, or of all groups.  The first 64 groups stay in the lanes.
+// Row tiles of a launch: of all rows, or of all groups, as many as the launch has workgroups for (groups that share rows could have so many that their number passes 32 bits).  The first 64
+// groups stay in the lanes.
 template <int R> struct MxTiles {
     MxGroupLane lane;
     int upto, total;
@@ -48,8 +49,10 @@ template <int R> struct MxTiles {
         if (!p.offsets) { total = (p.m + R - 1) / R; return; }
         lane = mx_group_lane<R>(p, threadIdx.x & 63);
         upto = mx_prefix(lane.tiles);
-        total = __builtin_amdgcn_readlane(upto, 63);
-        for (int g0 = 64; g0 < p.n_groups; g0 += 64) total += __builtin_amdgcn_readlane(mx_prefix(mx_group_lane<R>(p, g0 + (threadIdx.x & 63)).tiles), 63);
+        const int most = static_cast<int>(mx_most_row_tiles(p, R));
+        auto held = [&](int tiles) { return tiles < most ? tiles : most; };
+        total = held(__builtin_amdgcn_readlane(upto, 63));
+        for (int g0 = 64; g0 < p.n_groups; g0 += 64) total = held(total + __builtin_amdgcn_readlane(mx_prefix(mx_group_lane<R>(p, g0 + (threadIdx.x & 63)).tiles), 63));
     }
     __device__ __forceinline__ MxTile find(const MxOperands& p, int unit) const {
         if (!p.offsets) return {unit * R, 0, p.m, 0};

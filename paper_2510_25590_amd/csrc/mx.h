@@ -31,8 +31,8 @@ struct MxOperands {
     int m, n, row_bytes, steps;
 };
 
-// Row tiles of R rows that a launch may have: of groups, which begin at even rows, one more each.
-static inline int64_t mx_most_row_tiles(const MxOperands& p, int R) {
+// Row tiles of R rows that a launch may have: of groups, which begin at even rows, one more each.  Groups that share rows, against their contract, can have more: those beyond are not run.
+static __host__ __device__ inline int64_t mx_most_row_tiles(const MxOperands& p, int R) {
     if (!p.offsets) return (static_cast<int64_t>(p.m) + R - 1) / R;
     return p.m / R + (p.n_groups < p.m ? p.n_groups : p.m);
 }
