@@ -245,11 +245,13 @@ def check_asm(asm: str) -> None:
     for name, lines in _kernel_bodies(asm, "gemm_"):
         n += 1
         text = "\n".join(lines)
+        m = re.search(r"; ScratchSize: (\d+)", asm[asm.index(name + ":"):])
         if _COPY in text:
-            m = re.search(r"; ScratchSize: (\d+)", asm[asm.index(name + ":"):])
             if m and int(m.group(1)) != 0:
                 problems.append(f"{name[:70]}: uses {m.group(1)} bytes of scratch memory (its accesses share the copies' counter)")
             problems += check_copies(name, lines)
+        elif "gemm_mx_" in name and (m is None or int(m.group(1)) != 0):
+            problems.append(f"{name[:70]}: uses {m.group(1) if m else 'an unknown number of'} bytes of scratch memory (sums and loads ahead are meant to stay in registers)")
         problems += check_wide_stores(name, lines)
         problems += check_function(name, lines)
     if n == 0:
