@@ -287,7 +287,8 @@ int regione_linear_mxfp4(regione_ctx* ctx, const void* xq, const void* x_scale, 
  * starts is empty, and a group whose weight is not in [0, n_weights) is left out.  No two groups may share a row: if
  * they do, parts of that row come out as any of theirs, and rows of any group may stay as they were.  At most 65536
  * groups, m at most 2^24, n and k as for regione_linear_mxfp4.
- *   regione_linear_grouped: x bf16 [m, k], k a multiple of 64, weights of regione_pack_weight. */
+ *   regione_linear_grouped: x bf16 [m, k], k a multiple of 64, weights of regione_pack_weight.
+ * Here and in regione_linear_mxfp4 the activation may differ from regione_linear's by two units of float32's last place. */
 int regione_linear_grouped(regione_ctx* ctx, const void* x, const void* w_packed, const float* b_opt, const int32_t* group_offsets,
                            const int32_t* group_weight_opt, int32_t n_groups, int32_t n_weights, int32_t m, int32_t n, int32_t k,
                            int32_t act, int32_t out_dtype, void* y);

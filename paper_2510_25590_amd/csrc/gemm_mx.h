@@ -79,8 +79,8 @@ __device__ __forceinline__ f32x4 mx_mfma(const u32x4& w, const u32x4& a, const f
 }
 
 // 0.5 x (1 + tanh(u)) as in gelu_tanh_f32, without the correction of its quotient: 1.5 units of the last place of float32 from the reciprocal and the product, no more than what the rounded
-// argument of the exponential brings.  The end of a product in 4 bits is bound by these instructions: 820 x 12288 x 3072 31.9 -> 28.4 us, 25.8 without
-// activation.
+// argument of the exponential brings.  The end of a product in 4 bits is bound by these instructions; us with the correction / without it / without activation: 820 x 12288 x 3072
+// 25.9 / 24.4 / 21.2; with / without it: 16384 x 4096 x 2048 in 16 groups 103.7 / 99.6, 2000 x 2048 x 1024 in 16 groups of bf16 21.1 / 20.6.
 __device__ __forceinline__ float mx_gelu(float x) {
     constexpr float kLin = -2.0f * 0.7978845608028654f * 1.4426950408889634f, kCub = kLin * 0.044715f;
     const float e = __builtin_amdgcn_exp2f(x * __builtin_fmaf(x * x, kCub, kLin));
@@ -138,8 +138,8 @@ __device__ __forceinline__ void mx_put(const GemmEpilogue& ep, int row, int col,
 // Few rows: a wave owns 16 rows x 16 * CF columns of a part of K and reads its operands straight from memory, the weights as they lie, with the loads of CHUNK steps in flight.  KW of a
 // workgroup's eight waves share K and meet in LDS, where the sums are formed in wave order; the others take further columns.  Such a launch is a chain of trips to memory and the reading of
 // the weights.  Where K is long and N short there are fewer workgroups than CUs, and registers for one trip only: 16 columns, eight steps at a time, two waves per SIMD; us, 32 columns and
-// two steps / so: one row x 3072 x 12288 9.3 / 7.2 (the weights at 6.4 TB/s and the launch), 16 rows x 3072 x 15360 13.7 / 9.5, but one row x 9216 x 3072 5.8 / 7.6, 96 rows x 2048 x 1024 of
-// 64 experts 15.8 / 46.6.
+// two steps / so, weights in the Infinity Cache: one row x 3072 x 12288 6.7 / 5.0 (from HBM 8.8 / 6.9, 3 TB/s with the launch), 16 rows x 3072 x 15360 10.7 / 8.0, but one row x 9216 x 3072
+// 5.3 / 6.6, 96 rows x 2048 x 1024 of 64 experts 15.8 / 46.6.
 constexpr int kMxSmallRows = 16, kMxSmallWaves = 8;
 
 template <int FMT, int KW, int CF>

@@ -27,18 +27,21 @@ int launch_small(regione_ctx* ctx, int code, const MxOperands& p, const GemmEpil
 // ---- which kernel a product gets
 //
 // A plan's time is estimated as a start, whole and partial loads of the chip by workgroups (a fixed part and a part per step of K, which grow with the workgroups that share a CU, and the
-// activation, which they do one after the other), what the weights take from HBM (the root of both squares: the longer of them, and a little for the other), and the results' way out; a K split
+// activation, which they do one after the other), what the weights take (the root of both squares: the longer of them, and a little for the other), and the results' way out; a K split
 // adds its sums' way out and back, the kernel of 16 rows what its repeated reading of the weights takes.  The host does not know the groups' sizes: they are taken as random (exponentially distributed), a group of mean length s then has
 // 1 / (1 - exp(-R / s)) tiles of R rows.  All constants are fitted to every tile, K split and number of waves of 1978 products in 4 bits and 1312 in bf16 (1-16384 rows, 64-14400 columns,
 // K 256-16000, up to 64 groups, equal and random, with and without activation): over 990 / 657 others the choice is 1.9 / 2.3 % behind the best plan measured on average, 9 / 11 % in the
 // twentieth of them where it is furthest, 35 % at most (groups whose sizes are far from the assumed ones).
-// us, another tile / the choice: 820 x 12288 x 3072 256 x 256 32.0 / 192 x 256 25.8; 820 x 3072 x 12288 256 x 256 61.7 / 128 x 128 27.4; 128 x 3072 x 12288 unsplit 19.8 / four K splits
-// 13.7; 8704 x 12288 x 3072 128 x 128 204 / 128 x 256 172; one row x 9216 x 3072 all waves over columns 9.8 / four over K 5.2.
+// The products of the fit found their weights in the Infinity Cache (the 11 to 12 TB/s below), where a program that goes through many weights finds them in HBM.  Of 42 other products there the
+// choice was 0.8 % behind the best plan on average without groups, 25 % at most (205 x 3072 x 12288), and 9 % with groups, 40 % at most (two of 64 rows x 12288 x 3072 in bf16: 43.2 us, 64 x 128 tiles
+// 30.9); with weights in the cache 0.5 % and 7 %, 29 % at most (32 groups of three rows: equal groups are not what the estimate assumes).
+// us, another tile / the choice, weights in the cache: 820 x 12288 x 3072 224 x 256 23.9 / 192 x 256 20.7; 820 x 3072 x 12288 192 x 256 48.7 / 96 x 128 22.3; 128 x 3072 x 12288 unsplit 11.9 / two K
+// splits 9.9; 8704 x 12288 x 3072 128 x 128 197 / 128 x 256 165; one row x 9216 x 3072 all waves over columns 9.3 / eight over K 5.3 (four 5.2).
 // Left out, a kernel would cost the products that it is best for: the one of 16 rows with one, two, four and eight waves over K 32, 7, 18 and 48 %, with 16 columns 49 %.
 struct MxPlan { int tile, splits; };      // tile 1, 2, 4, 8: the kernel of 16 rows and 32 columns per wave with as many waves over K; 9: with eight, 16 columns
 struct MxTileCost { int code, per_cu; double fixed, step, more; };               // us, us per step, and what each further workgroup of a CU adds to the latter (as a share)
 struct MxSmallCost { int code; double fixed, step, work; };                       // us and us per step of a wave, per load of the chip; us per 1e5 steps of columns
-struct MxCosts { MxTileCost tile[11]; MxSmallCost small[5]; double start, hbm, out, gelu; };     // us, bytes of weights per us, results per us, us per 100 kB of a tile's sums
+struct MxCosts { MxTileCost tile[11]; MxSmallCost small[5]; double start, weights, out, gelu; }; // us, bytes of weights per us, results per us, us per 100 kB of a tile's sums
 constexpr MxCosts kMxCosts[2] = {
     {{{72, 1, 2.82, 0.922, 0.000}, {62, 1, 2.37, 0.799, 0.000}, {52, 1, 2.46, 0.597, 0.000}, {42, 2, 1.36, 0.505, 1.118}, {32, 2, 0.90, 0.434, 1.148}, {51, 2, 0.98, 0.384, 1.119},
       {41, 2, 0.82, 0.295, 1.348}, {31, 3, 0.57, 0.243, 1.305}, {22, 2, 0.47, 0.344, 1.268}, {21, 3, 0.30, 0.202, 1.312}, {11, 3, 0.45, 0.164, 1.420}},
@@ -56,7 +59,7 @@ double row_tiles_expected(const MxOperands& p, int R) {
 MxPlan choose(int fmt, const MxOperands& p, int act, size_t part_bytes) {
     const MxCosts& c = kMxCosts[fmt];
     const int groups = p.offsets ? p.n_groups : 1;
-    const double weights = static_cast<double>(p.m < groups ? p.m : groups) * p.n * p.steps * (fmt == MX_FP4 ? 136.0 : 128.0) / c.hbm;
+    const double weights = static_cast<double>(p.m < groups ? p.m : groups) * p.n * p.steps * (fmt == MX_FP4 ? 136.0 : 128.0) / c.weights;
     MxPlan best = {42, 1};
     double best_us = 1e30;
     auto consider = [&](int tile, int splits, double us) { if (us < best_us) { best_us = us; best = {tile, splits}; } };

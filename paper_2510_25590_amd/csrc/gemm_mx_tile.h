@@ -5,9 +5,12 @@
 // LOOK steps ahead and registers are loaded again as soon as they have been used.  A step is four phases of RF * CF instructions; while a phase's instructions run, the same wave reads the
 // rows of the next phase, puts rows of the next step into LDS and requests rows, weights and scales of the steps ahead.  One barrier per step.
 // Why not straight into LDS: such copies are taken at 35 bytes a clock by a CU (all tiles ended at 65 to 70 bytes a ns), where loads into registers get 64; and
-// weights in LDS, shared by waves that split the rows, cost it as many bytes again.  us, tiles of the same sizes with copies into LDS / now: 820 x 3072 x 12288 30.0 / 27.6,
-// 205 x 12288 x 3072 12.5 / 11.4, 64 x 9216 x 3072 6.9 / 6.2, 128 x 3072 x 12288 23.6 / 20.0, 2048 x 8192 x 12288 106 / 97.  A large product is then bound by power: 128 x 256 tiles of
-// 8704 x 12288 x 3072 run at 3.8 PFLOP/s, the matrix instructions busy at 1.8 to 1.9 GHz; a small one by the weights from HBM and the trips there.
+// weights in LDS, shared by waves that split the rows, cost it as many bytes again.  us, tiles of the same sizes with copies into LDS / so: 820 x 3072 x 12288 30.0 / 27.6,
+// 205 x 12288 x 3072 12.5 / 11.4, 64 x 9216 x 3072 6.9 / 6.2, 128 x 3072 x 12288 23.6 / 20.0, 2048 x 8192 x 12288 106 / 97.
+// What bounds it.  Several rounds of tiles (8704 x 9216 x 3072, 127 us, 3.9 PFLOP/s): matrix instructions run in 63 % of the cycles in which a CU holds workgroups, at 1.6 to 1.8 GHz, where a register loop that is
+// always busy holds 1.55 (6.5 PFLOP/s); in the rest the two workgroups of a CU, which run in step, start, end or wait together, and the 4.8 rounds of tiles take the time of five.  One round
+// (820 x 12288 x 3072): the start and the end, which nothing hides, are half of the call.  128 columns: all four waves read all rows, so a step of 160 x 128 moves 100 KiB through LDS, 800
+// clocks at 128 bytes, beside 640 of matrix instructions; the counters have each busy 52 % of the time (1382 x 3072 x 15360), and a second workgroup per CU finds nothing left to overlap.
 // The 32x32 instruction reaches its rate with one wave per SIMD, which the 16x16 one does not (register-only loops in 4 bits, PFLOP/s with one, two and four waves per
 // SIMD: 6.3 / 6.5 / 6.6 against 4.2 / 5.5 / 6.1).
 #pragma once
