@@ -296,6 +296,61 @@ int regione_linear_mxfp4_grouped(regione_ctx* ctx, const void* xq, const void* x
                                  const int32_t* group_offsets, const int32_t* group_weight_opt, int32_t n_groups, int32_t n_weights,
                                  int32_t m, int32_t n, int32_t k, int32_t act, int32_t out_dtype, void* y);
 
+/* A router's products over groups of rows: which experts a token gets, the rows sorted by expert (groups for
+ * regione_linear_grouped and regione_linear_mxfp4_grouped), and the experts' results back at their tokens.  A routed layer is
+ *   regione_linear (logits, float32) -> regione_expert_route -> regione_expert_slots -> regione_gather(x, index = row_token,
+ *   n_dev = group_offsets + n_experts, n_max = n_tokens * top_k) -> regione_linear_grouped (x2) -> regione_expert_combine.
+ * An extension: editors whose MLPs are mixtures of experts need it, the paper keeps its DiT a black box.  Nothing waits
+ * for the host.  At most 1024 experts, 32 choices per token and 2^24 choices in all (as tokens); the same in every context type.
+ *
+ * regione_expert_route: logits [n_tokens, n_experts] of `dtype`.
+ *   score s = softmax of the token's logits or sigmoid of each; value c = s + bias[expert] (bias_opt [n_experts] float32: a
+ *   balance between experts that decides who is chosen and is not part of the weight), in float64.
+ *   n_groups > 1: expert e belongs to group e / (n_experts / n_groups); a group's value is the sum of its group_best (1 or 2)
+ *   largest c (of the only one if it has one), the top_groups groups of the largest values stay.
+ *   expert [n_tokens, top_k] int32: the experts of the largest c in falling order, of equal ones the lowest first, for groups as
+ *   well; without a bias experts are compared by their logits, which the scores grow with.  An expert whose logit or value is NaN
+ *   or -infinity is never chosen; a logit of +infinity counts as the largest float32.
+ *   weight [n_tokens, top_k] float32: scale * s, with `renormalise` scale * s / (sum of the token's chosen s; 0 if that is 0).
+ *   Where fewer than top_k experts can be chosen the last entries are expert -1, weight 0; so are all entries of a token
+ *   whose mask_opt [n_tokens] uint8 is 0.
+ *   n_groups divides n_experts (at most 64 groups), top_k <= top_groups * n_experts / n_groups.
+ * regione_expert_slots: a stable sort of the pairs (token, j) by expert[token, j]; entries outside [0, n_experts) belong to none.
+ *   group_offsets [n_experts + 1] int32: first row of every expert, and the end;  row_token [n_tokens * top_k] int32: the token
+ *   of each row, ascending within an expert (entries past the end stay as they were);  slot [n_tokens, top_k] int32: the
+ *   row of each pair, -1 for none.
+ * regione_expert_combine: out[t] = base[t] + sum over j of weight[t, j] * rows[slot[t, j]], in float32 in the order of j, rounded
+ *   once; slots outside [0, n_rows) add nothing.  rows [n_rows, cols] of rows_dtype; weight_opt NULL: 1; base_opt
+ *   [n_tokens, cols] of out_dtype, may be `out` itself, NULL: 0; out [n_tokens, cols] of out_dtype.  rows and out must not overlap. */
+enum { REGIONE_SCORE_SOFTMAX = 0, REGIONE_SCORE_SIGMOID = 1 };
+int regione_expert_route(regione_ctx* ctx, const void* logits, int32_t dtype, const float* bias_opt, const uint8_t* mask_opt,
+                         int64_t n_tokens, int32_t n_experts, int32_t score, int32_t n_groups, int32_t top_groups, int32_t group_best,
+                         int32_t top_k, int32_t renormalise, float scale, int32_t* expert, float* weight);
+int regione_expert_slots(regione_ctx* ctx, const int32_t* expert, int64_t n_tokens, int32_t top_k, int32_t n_experts,
+                         int32_t* group_offsets, int32_t* row_token, int32_t* slot);
+int regione_expert_combine(regione_ctx* ctx, const void* rows, int32_t rows_dtype, int64_t n_rows, const int32_t* slot,
+                           const float* weight_opt, const void* base_opt, int64_t n_tokens, int32_t top_k, int32_t cols,
+                           int32_t out_dtype, void* out);
+
+/* regione_linear with low-rank adapters beside the projection, n_sel of n_adapters for every row:
+ *   y[r] = act(x[r] W^T + b + sum over s of weight[r, s] * (x[r] A_a^T) B_a^T),   a = adapter[r, s],
+ * the rows of a batch of requests each with its own adapters, or, with the experts and weights of regione_expert_route as they
+ * are, a mixture of low-rank experts.
+ *   adapter [m, n_sel] int32 on the device: entries outside [0, n_adapters) (-1) add nothing, the same one twice adds twice;
+ *   weight_opt [m, n_sel] float32, NULL: 1;
+ *   adapters_packed: n_adapters packed adapters one after the other, each of regione_packed_adapter_elems(n, k, rank) bf16
+ *   elements, made by regione_pack_adapter from A [rank, k] and B [n, rank] (bf16 row-major; smaller adapters padded with
+ *   zeros to the common rank); they must be 16-byte aligned.
+ *   k a multiple of 64; rank 1..256, n_sel 1..32, n_adapters at most 65536.  bf16 contexts.
+ * x A^T is summed in float32, multiplied by its weight and kept as two (y in bf16) or three (y in float32) bf16 terms, to 2^-16
+ * and to float32's own precision.  An adapter whose values are not finite spoils the rows that use it, and no others.  Uses the context's
+ * workspace (REGIONE_ERR_WORKSPACE in a context without max_fresh). */
+int64_t regione_packed_adapter_elems(int32_t n, int32_t k, int32_t rank);
+int regione_pack_adapter(regione_ctx* ctx, const void* a, const void* b, int32_t n, int32_t k, int32_t rank, void* packed);
+int regione_linear_adapters(regione_ctx* ctx, const void* x, const void* w_packed, const float* b_opt, const void* adapters_packed,
+                            const int32_t* adapter, const float* weight_opt, int32_t n_adapters, int32_t n_sel, int32_t rank,
+                            int32_t m, int32_t n, int32_t k, int32_t act, int32_t out_dtype, void* y);
+
 /* One transformer block on the fresh rows: one layer of Phi(tokens, C_KV, f) in
  * Algorithm 1.  The block is LayerNorm (no affine, eps 1e-6) -> modulation -> QKV linear ->
  * attention -> gated residual -> LayerNorm -> modulation -> MLP with tanh-GELU -> gated

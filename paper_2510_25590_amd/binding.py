@@ -21,6 +21,7 @@ BLOCK_DOUBLE, BLOCK_SINGLE = 0, 1
 FLAG_STORE, FLAG_RETRIEVE = 1, 2
 ACT_NONE, ACT_GELU_TANH, ACT_SILU = 0, 1, 2
 MX_SCALE_ROWS, MX_SCALE_STEPS = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 
 EXPORTS = (
     "regione_last_error", "regione_create", "regione_destroy", "regione_partition", "regione_gather",
@@ -37,6 +38,7 @@ EXPORTS = (
     "regione_tune_attention_form", "regione_attention_workgroups",
     "regione_mxfp4_scale_bytes", "regione_quantize_rows_mxfp4", "regione_dequantize_rows_mxfp4", "regione_packed_weight_mxfp4_bytes",
     "regione_pack_weight_mxfp4", "regione_linear_mxfp4", "regione_linear_grouped", "regione_linear_mxfp4_grouped", "regione_tune_mx",
+    "regione_expert_route", "regione_expert_slots", "regione_expert_combine", "regione_packed_adapter_elems", "regione_pack_adapter", "regione_linear_adapters",
 )
 STEP_FULL, STEP_FULL_STORE, STEP_REGION = 0, 1, 2
 PROF_NAMES = ("partition", "rows", "layernorm", "gemm", "attention", "velocity")
@@ -164,6 +166,12 @@ def lib() -> C.CDLL:
             "regione_linear_grouped": [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp],
             "regione_tune_mx": [vp, i32, i32],
             "regione_linear_mxfp4_grouped": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp],
+            "regione_expert_route": [vp, vp, i32, vp, vp, i64, i32, i32, i32, i32, i32, i32, i32, f32, vp, vp],
+            "regione_expert_slots": [vp, vp, i64, i32, i32, vp, vp, vp],
+            "regione_expert_combine": [vp, vp, i32, i64, vp, vp, vp, i64, i32, i32, i32, vp],
+            "regione_packed_adapter_elems": [i32, i32, i32],
+            "regione_pack_adapter": [vp, vp, vp, i32, i32, i32, vp],
+            "regione_linear_adapters": [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, vp],
             "regione_tune_gemm": [vp, i32, i32],
             "regione_block_lanes_host": [i32, i32, i32, i32, i32, C.POINTER(i32)],
             "regione_tune_attention": [vp, i32],
@@ -187,6 +195,7 @@ def lib() -> C.CDLL:
         _lib.regione_packed_weight_elems.argtypes = [i32, i32]
         _lib.regione_packed_weight_elems.restype = C.c_int64
         _lib.regione_mxfp4_scale_bytes.restype = _lib.regione_packed_weight_mxfp4_bytes.restype = C.c_int64
+        _lib.regione_packed_adapter_elems.restype = C.c_int64
     return _lib
 
 
@@ -604,6 +613,49 @@ def pack_weight_mxfp4(ctx, w):
         q, scale = quantize_rows_mxfp4(ctx, w, MX_SCALE_ROWS)
         out = torch.empty(regione_packed_weight_mxfp4_bytes(n, k), dtype=torch.uint8, device=w.device)
         regione_pack_weight_mxfp4(ctx, q, scale, n, k, out)
+        results.append(out)
+    return out
+
+
+def regione_expert_route(ctx, logits, dtype, bias, mask, n_tokens, n_experts, score, n_groups, top_groups, group_best, top_k, renormalise, scale, expert, weight):
+    _check(lib().regione_expert_route(ctx.handle, _p(logits), dtype, _p(bias), _p(mask), n_tokens, n_experts, score, n_groups, top_groups, group_best, top_k,
+                                      int(bool(renormalise)), float(scale), _p(expert), _p(weight)))
+
+
+def regione_expert_slots(ctx, expert, n_tokens, top_k, n_experts, group_offsets, row_token, slot):
+    _check(lib().regione_expert_slots(ctx.handle, _p(expert), n_tokens, top_k, n_experts, _p(group_offsets), _p(row_token), _p(slot)))
+
+
+def regione_expert_combine(ctx, rows, rows_dtype, n_rows, slot, weight, base, n_tokens, top_k, cols, out_dtype, out):
+    _check(lib().regione_expert_combine(ctx.handle, _p(rows), rows_dtype, n_rows, _p(slot), _p(weight), _p(base), n_tokens, top_k, cols, out_dtype, _p(out)))
+
+
+def regione_packed_adapter_elems(n: int, k: int, rank: int) -> int:
+    return int(lib().regione_packed_adapter_elems(n, k, rank))
+
+
+def regione_pack_adapter(ctx, a, b, n, k, rank, packed):
+    _check(lib().regione_pack_adapter(ctx.handle, _p(a), _p(b), n, k, rank, _p(packed)))
+
+
+def regione_linear_adapters(ctx, x, w_packed, b, adapters_packed, adapter, weight, n_adapters, n_sel, rank, m, n, k, act, out_dtype, y):
+    _check(lib().regione_linear_adapters(ctx.handle, _p(x), _p(w_packed), _p(b), _p(adapters_packed), _p(adapter), _p(weight), n_adapters, n_sel, rank,
+                                         m, n, k, act, out_dtype, _p(y)))
+
+
+def pack_adapters(ctx, a, b):
+    """Convenience: packs the adapters A [n_adapters, rank, k] and B [n_adapters, n, rank], bf16 CUDA tensors, into a new tensor in the library's layout."""
+    import torch
+    shapes = a.dim() == 3 and b.dim() == 3 and a.shape[0] == b.shape[0] and a.shape[1] == b.shape[2]
+    for t in (a, b):
+        if not shapes or t.dtype != torch.bfloat16 or t.device != ctx.stream.device:
+            raise RegionEError(ERR_INVALID_ARG, f"pack_adapters: {a.dtype} {tuple(a.shape)} on {a.device} and {b.dtype} {tuple(b.shape)} on {b.device}, "
+                                                f"not bf16 [n_adapters, rank, k] and [n_adapters, n, rank] on {ctx.stream.device}")
+    (count, rank, k), n = a.shape, b.shape[1]
+    with _on_stream_of(ctx, a, b) as results:
+        out = torch.empty((count, regione_packed_adapter_elems(n, k, rank)), dtype=torch.bfloat16, device=a.device)
+        for i in range(count):
+            regione_pack_adapter(ctx, a[i].contiguous(), b[i].contiguous(), n, k, rank, out[i])
         results.append(out)
     return out
 

@@ -1,6 +1,6 @@
 // GEMM kernel in which two groups of waves alternate between memory work and matrix-core work (gemm_pp_kernel below).
 #pragma once
-#include "gemm_epilogue.h"
+#include "gemm_adapters.h"
 
 namespace {
 
@@ -120,7 +120,12 @@ __device__ __forceinline__ void pp_finish(f32x4 (&acc)[RF][CF], unsigned char* l
                 if (s + 1 < splits) add(1, h, s + 1);
             }
     }
-    gemm_epilogue16<KIND, FP8, I0, I1, RF, CF>(acc, M, N, m0, n0w, ep);
+    if constexpr (KIND == EPI_ADAPTERS) {
+        adapters_add<I0, I1, RF, CF>(acc, M, N, m0, n0w, ep.adapters);
+        gemm_epilogue16<EPI_PLAIN, FP8, I0, I1, RF, CF>(acc, M, N, m0, n0w, ep);
+    } else {
+        gemm_epilogue16<KIND, FP8, I0, I1, RF, CF>(acc, M, N, m0, n0w, ep);
+    }
 }
 
 // RF x CF fragments of 16 x 16 per wave, 2 x 4 waves: 32*RF rows x 64*CF columns per workgroup.

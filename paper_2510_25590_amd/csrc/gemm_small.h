@@ -8,7 +8,7 @@
 // Which products come here, and what they took before: small_columns (gemm.hip).  In a block of width 256 and 36 rows the launch of a LayerNorm and that of
 // its product took 3.4 + 5.4 us, one launch now 3.7; two such blocks with everything around them 85 -> 62 us.
 #pragma once
-#include "gemm_epilogue.h"
+#include "gemm_adapters.h"
 #include "layernorm_row.h"
 
 namespace {
@@ -33,7 +33,7 @@ static_assert(small_lds_bytes<4>(true, kLnColumns) <= 65536u, "what a launch may
 template <int CF, int KIND, int LN>
 __device__ __forceinline__ void gemm_small_tile(unsigned char* lds, int tile_y, const void* __restrict__ A, int lda, const bf16_t* __restrict__ Wp, int M, int N, int K,
                                                 const float* __restrict__ shift, const float* __restrict__ scale, const GemmEpilogue& ep) {
-    constexpr int CHUNK = SmallTile<CF>::CHUNK;
+    constexpr int CHUNK = SmallTile<CF>::CHUNK, END = KIND == EPI_ADAPTERS ? EPI_PLAIN : KIND;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, quad = lane >> 4;
@@ -58,13 +58,13 @@ __device__ __forceinline__ void gemm_small_tile(unsigned char* lds, int tile_y, 
     // The launch is a chain of trips to memory: what the epilogue reads is requested first, by the waves that finish the tile (wave b block b of 32 columns)
     const int fin_col = n0 + 32 * wave + 8 * quad;
     const bool finishes = wave < CF / 2, whole = (ep.vec_ok || KIND != EPI_QKV) && fin_col + 8 <= N;
-    EpiColumns<KIND, false> fin_cols;
-    EpiRow<KIND, false> fin_row;
+    EpiColumns<END, false> fin_cols;
+    EpiRow<END, false> fin_row;
     Raw8 fin_raw;
     if (finishes && whole) {
         fin_row.load(ep, row);
         fin_cols.load(ep, fin_col);
-        if (epi_reads<KIND>()) fin_raw = ep.vec_ok ? epi_load8<KIND, true>(ep, row, fin_col) : epi_load8<KIND, false>(ep, row, fin_col);
+        if (epi_reads<END>()) fin_raw = ep.vec_ok ? epi_load8<END, true>(ep, row, fin_col) : epi_load8<END, false>(ep, row, fin_col);
     }
 
     f32x4 acc[CF];
@@ -111,6 +111,7 @@ __device__ __forceinline__ void gemm_small_tile(unsigned char* lds, int tile_y, 
                 for (int j = 0; j < CF; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i][j], a[i], acc[j], 0, 0, 0);
             }
     }
+    if constexpr (KIND == EPI_ADAPTERS) adapters_add<0, 1, 1, CF>(reinterpret_cast<f32x4(&)[1][CF]>(acc), M, N, m0, n0, ep.adapters, wave, kSmallWaves);
     if (LN != LN_NONE) __syncthreads();                         // the rows have been read
     f32x4* sums = reinterpret_cast<f32x4*>(lds) + lane;
 #pragma unroll
@@ -125,9 +126,9 @@ __device__ __forceinline__ void gemm_small_tile(unsigned char* lds, int tile_y, 
         for (int v = 1; v < kSmallWaves; ++v) sum[jl] += sums[(v * CF + 2 * wave + jl) * 64];
     }
     if (m0 + l16 >= M || fin_col >= N) return;
-    if (!whole) epilogue_ragged<KIND, false>(ep, row, fin_col, N, sum[0], sum[1]);
-    else if (ep.vec_ok) epilogue_store8<KIND, false, true>(ep, row, fin_col, sum[0], sum[1], fin_cols, fin_row, fin_raw);
-    else epilogue_store8<KIND, false, false>(ep, row, fin_col, sum[0], sum[1], fin_cols, fin_row, fin_raw);
+    if (!whole) epilogue_ragged<END, false>(ep, row, fin_col, N, sum[0], sum[1]);
+    else if (ep.vec_ok) epilogue_store8<END, false, true>(ep, row, fin_col, sum[0], sum[1], fin_cols, fin_row, fin_raw);
+    else epilogue_store8<END, false, false>(ep, row, fin_col, sum[0], sum[1], fin_cols, fin_row, fin_raw);
 }
 
 template <int CF, int KIND, int LN>
