@@ -9,6 +9,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMostExperts = 1024, kMostChosen = 32, kMostGroups = 64;
 constexpr int64_t kMostPairs = int64_t{1} << 24;             // rows that a grouped product takes
+constexpr int64_t kRouteShared = 16384;                      // tokens from which on four share a wave
 
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -17,38 +18,81 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 struct RouteCall {
     const void* logits; const float* bias; const uint8_t* mask; int32_t* expert; float* weight;
-    int64_t n_tokens; int n_experts, n_groups, top_groups, group_best, top_k, group_lanes;
+    int64_t n_tokens; int n_experts, n_groups, top_groups, group_best, top_k, per, group_shift;   // experts per group; a group's lanes are 1 << group_shift
     int sigmoid, renormalise, whole; float scale;            // whole: every lane's experts exist and lie at a multiple of their own size
 };
 
-// Lane exchange within LPT lanes (16: a DPP row; 64: the wave): v of the lane XOR 1, 2, 4, 8 by DPP, further ones through the LDS crossbar.
-template <int X> __device__ __forceinline__ int lane_xor(int v) {
+// Reductions over LPT lanes (16: a DPP row; 64: the wave) that leave the result in all of them.  Step X combines a lane with one of the other half of its 2 X lanes, whose X lanes agree by
+// then: which of them does not matter, so that mirrors serve where DPP has no exchange.  Nothing goes through the LDS crossbar, whose latency is ten times as long.
+template <int X> __device__ __forceinline__ int lane_across(int v) {
     if constexpr (X == 1) return __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true);              // quad_perm 1 0 3 2
     else if constexpr (X == 2) return __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true);         // quad_perm 2 3 0 1
-    else if constexpr (X == 4) return __builtin_amdgcn_ds_swizzle(v, 0x101f);
-    else if constexpr (X == 8) return __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, true);        // row_ror:8
-    else if constexpr (X == 16) return __builtin_amdgcn_ds_swizzle(v, 0x401f);
-    else return __builtin_amdgcn_ds_bpermute(((threadIdx.x & 63) ^ 32) * 4, v);
+    else if constexpr (X == 4) return __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);        // row_half_mirror
+    else if constexpr (X == 8) return __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true);        // row_mirror
+    else {
+        // the instruction exchanges the odd rows (the upper half) of one register with the even rows (the lower half) of the other
+        const auto both = X == 16 ? __builtin_amdgcn_permlane16_swap(v, v, false, false) : __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return static_cast<int>(threadIdx.x & X ? both[0] : both[1]);
+    }
 }
-template <int X> __device__ __forceinline__ float lane_xor(float v) { return __int_as_float(lane_xor<X>(__float_as_int(v))); }
-template <int X> __device__ __forceinline__ double lane_xor(double v) { return __hiloint2double(lane_xor<X>(__double2hiint(v)), lane_xor<X>(__double2loint(v))); }
+template <int X> __device__ __forceinline__ unsigned lane_across(unsigned v) { return static_cast<unsigned>(lane_across<X>(static_cast<int>(v))); }
+template <int X> __device__ __forceinline__ float lane_across(float v) { return __int_as_float(lane_across<X>(__float_as_int(v))); }
+template <int X> __device__ __forceinline__ double lane_across(double v) { return __hiloint2double(lane_across<X>(__double2hiint(v)), lane_across<X>(__double2loint(v))); }
+// both halves' values, in an order that is the same in all lanes
+template <int X> __device__ __forceinline__ void lane_halves(int v, int& a, int& b) {
+    const auto both = X == 16 ? __builtin_amdgcn_permlane16_swap(v, v, false, false) : __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    a = static_cast<int>(both[0]);
+    b = static_cast<int>(both[1]);
+}
+template <int X> __device__ __forceinline__ void lane_halves(unsigned v, unsigned& a, unsigned& b) { lane_halves<X>(static_cast<int>(v), reinterpret_cast<int&>(a), reinterpret_cast<int&>(b)); }
+template <int X> __device__ __forceinline__ void lane_halves(float v, float& a, float& b) {
+    int x, y;
+    lane_halves<X>(__float_as_int(v), x, y);
+    a = __int_as_float(x);
+    b = __int_as_float(y);
+}
+template <int X> __device__ __forceinline__ void lane_halves(double v, double& a, double& b) {
+    int ah, al, bh, bl;
+    lane_halves<X>(__double2hiint(v), ah, bh);
+    lane_halves<X>(__double2loint(v), al, bl);
+    a = __hiloint2double(ah, al);
+    b = __hiloint2double(bh, bl);
+}
 template <int X, int LPT, typename V, typename F> __device__ __forceinline__ V over_lanes(V v, F f) {
-    if constexpr (X < LPT) return over_lanes<2 * X, LPT>(f(v, lane_xor<X>(v)), f);
-    else return v;
+    if constexpr (X >= LPT) {
+        return v;
+    } else if constexpr (X < 16) {
+        return over_lanes<2 * X, LPT>(f(v, lane_across<X>(v)), f);
+    } else {
+        V a, b;
+        lane_halves<X>(v, a, b);
+        return over_lanes<2 * X, LPT>(f(a, b), f);
+    }
 }
 __device__ __forceinline__ float bigger(float a, float b) { return __builtin_fmaxf(a, b); }
 __device__ __forceinline__ double bigger(double a, double b) { return __builtin_fmax(a, b); }
+__device__ __forceinline__ unsigned bigger(unsigned a, unsigned b) { return a > b ? a : b; }
+__device__ __forceinline__ float smaller(float a, float b) { return __builtin_fminf(a, b); }
+__device__ __forceinline__ double smaller(double a, double b) { return __builtin_fmin(a, b); }
+__device__ __forceinline__ unsigned smaller(unsigned a, unsigned b) { return a < b ? a : b; }
 template <int LPT, typename V> __device__ __forceinline__ V lanes_max(V v) { return over_lanes<1, LPT>(v, [](V a, V b) { return bigger(a, b); }); }
+template <int LPT, typename V> __device__ __forceinline__ V lanes_min(V v) { return over_lanes<1, LPT>(v, [](V a, V b) { return smaller(a, b); }); }
 template <int LPT, typename V> __device__ __forceinline__ V lanes_sum(V v) { return over_lanes<1, LPT>(v, [](V a, V b) { return a + b; }); }
+// of lane `from`, the same number for all lanes of the token
+template <int LPT> __device__ __forceinline__ int lane_value(int v, int from) {
+    if constexpr (LPT == 64) return __builtin_amdgcn_readlane(v, from);
+    else return __builtin_amdgcn_ds_bpermute(from * 4, v);
+}
+template <int LPT> __device__ __forceinline__ float lane_value(float v, int from) { return __int_as_float(lane_value<LPT>(__float_as_int(v), from)); }
+template <int LPT> __device__ __forceinline__ double lane_value(double v, int from) { return __hiloint2double(lane_value<LPT>(__double2hiint(v), from), lane_value<LPT>(__double2loint(v), from)); }
 
 // Two largest values of the lanes of a group (1 to LPT lanes).
-template <int X, int LPT> __device__ __forceinline__ void best_two(double& a, double& b, int lanes) {
+template <int X, int LPT, typename V> __device__ __forceinline__ void best_two(V& a, V& b, int lanes) {
     if constexpr (X < LPT) {
-        const double oa = lane_xor<X>(a), ob = lane_xor<X>(b);
-        if (X < lanes) {
-            b = bigger(__builtin_fmin(a, oa), bigger(b, ob));
-            a = bigger(a, oa);
-        }
+        if (X >= lanes) return;
+        const V oa = lane_across<X>(a), ob = lane_across<X>(b);
+        b = bigger(smaller(a, oa), bigger(b, ob));
+        a = bigger(a, oa);
         best_two<2 * X, LPT>(a, b, lanes);
     }
 }
@@ -57,112 +101,205 @@ template <typename T> __device__ __forceinline__ float as_float(T v);
 template <> __device__ __forceinline__ float as_float<float>(float v) { return v; }
 template <> __device__ __forceinline__ float as_float<bf16_t>(bf16_t v) { return bf16_to_f32(v); }
 
-// LPT lanes choose the experts of a token.  A group has LPT / (n_groups rounded up to a power of two) lanes of EPL experts each, in order, so that among equal values the lowest lane and
-// then its lowest place hold the lowest expert.
-// Which expert is chosen is decided in 64 bits wherever a score takes part (EXACT: with a bias, or sums of two scores over a group): in 32 bits the rounding of the exponential would
-// decide between experts that differ by less, and another order of the same operations would choose others.  Without either the scores lie in the order of the logits.
-template <typename T, int LPT, int EPL, bool EXACT>
-__global__ void __launch_bounds__(kThreads)
-route_kernel(RouteCall c) {
-    typedef typename std::conditional<EXACT, double, float>::type V;
-    constexpr V NONE = static_cast<V>(-INFINITY);
-    const int lane = threadIdx.x & 63, l = lane & (LPT - 1);
-    const int64_t token = (static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6)) * (64 / LPT) + lane / LPT;
-    if (token - lane / LPT >= c.n_tokens) return;                          // (the whole wave)
-    const bool there = token < c.n_tokens, routed = there && (!c.mask || c.mask[token] != 0);
-    const int group_lanes = c.group_lanes, group = l / group_lanes, per = c.n_experts / c.n_groups, first = (l & (group_lanes - 1)) * EPL;
-    const int expert0 = group * per + first;                               // of this lane
-    int mine = group < c.n_groups ? per - first : 0;                       // its experts
-    mine = mine < 0 ? 0 : (mine < EPL ? mine : EPL);
-
-    float logit[EPL];
-    V value[EPL];
-    const T* row = static_cast<const T*>(c.logits) + (routed ? token : 0) * c.n_experts;
-    if (c.whole) {
-        typedef T piece __attribute__((ext_vector_type(EPL * sizeof(T) > 16 ? 16 / sizeof(T) : EPL)));
-        constexpr int PE = sizeof(piece) / sizeof(T);
-        piece p[EPL / PE];
-        const bool any = group < c.n_groups;
-#pragma unroll
-        for (int i = 0; i < EPL / PE; ++i) p[i] = reinterpret_cast<const piece*>(row + (any ? expert0 : 0))[i];
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-            T v;
-            if constexpr (PE == 1) v = reinterpret_cast<const T*>(p)[i]; else v = p[i / PE][i % PE];
-            logit[i] = any ? as_float<T>(v) : -INFINITY;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) logit[i] = i < mine ? as_float<T>(row[expert0 + i]) : -INFINITY;
+// A value and its expert as one number, larger for larger values and, among equal ones, for lower experts: a maximum finds both at once.  Float32 values are put into the upper bits of
+// a double, whose lowest ten hold the expert; bf16 values into the upper half of a word.  A value of -infinity is no expert.
+struct WideKey {
+    typedef double type;
+    static constexpr double NONE = -INFINITY;
+    static __device__ __forceinline__ double make(float v, int expert) {
+        v += 0.0f;                                                         // (-0 is as large as 0)
+        const double d = static_cast<double>(v);
+        const int low = (1023 - expert) ^ ((__float_as_int(v) >> 31) & 1023);
+        return __hiloint2double(__double2hiint(d), v > -INFINITY ? __double2loint(d) | low : 0);
     }
-    // NaN is no score at all; what overflows counts as the largest value there is
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) logit[i] = logit[i] > -INFINITY ? __builtin_fminf(logit[i], 3.402823466e38f) : -INFINITY;
-
-    float top = logit[0];
-#pragma unroll
-    for (int i = 1; i < EPL; ++i) top = bigger(top, logit[i]);
-    top = lanes_max<LPT>(top);
-    double all = 0.0;                                                      // sum of the softmax's exponentials
-    if constexpr (EXACT) {
-        double e[EPL];
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) e[i] = logit[i] == -INFINITY ? 0.0 : exp(c.sigmoid ? -static_cast<double>(logit[i]) : static_cast<double>(logit[i]) - static_cast<double>(top));
-        if (!c.sigmoid) {
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) all += e[i];
-            all = lanes_sum<LPT>(all);
-        }
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-            double v = c.sigmoid ? 1.0 / (1.0 + e[i]) : e[i] / all;
-            if (c.bias && i < mine) v += static_cast<double>(c.bias[expert0 + i]);
-            value[i] = logit[i] > -INFINITY && v > NONE ? v : NONE;        // (a bias of NaN or -infinity takes its expert out)
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) value[i] = logit[i];
-        if (!c.sigmoid && !c.renormalise) {
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) sum += logit[i] == -INFINITY ? 0.f : expf(logit[i] - top);
-            all = lanes_sum<LPT>(sum);
-        }
+    static __device__ __forceinline__ int expert(double k) { return 1023 - ((__double2loint(k) & 1023) ^ ((__double2hiint(k) >> 31) & 1023)); }
+    static __device__ __forceinline__ float value(double k) { return static_cast<float>(__hiloint2double(__double2hiint(k), __double2loint(k) & ~1023)); }
+};
+struct NarrowKey {
+    typedef unsigned type;
+    static constexpr unsigned NONE = 0;
+    static __device__ __forceinline__ unsigned make(float v, int expert) {
+        unsigned bits = __float_as_uint(v);
+        bits = bits == 0x80000000u ? 0u : bits;                            // (-0 is as large as 0)
+        const unsigned ordered = bits ^ (static_cast<unsigned>(static_cast<int>(bits) >> 31) | 0x80000000u);
+        return v > -INFINITY ? (ordered & 0xffff0000u) | static_cast<unsigned>(1023 - expert) : NONE;
     }
+    static __device__ __forceinline__ int expert(unsigned k) { return 1023 - static_cast<int>(k & 1023u); }
+    static __device__ __forceinline__ float value(unsigned k) {
+        const unsigned bits = k >> 16;
+        return __uint_as_float((bits & 0x8000u ? bits & 0x7fffu : ~bits & 0xffffu) << 16);
+    }
+};
 
-    if (EXACT && c.n_groups > 1) {
-        // A group's place is the number of groups that come before it: those with more, and those with as much and a lower number.
-        double a = NONE, b = NONE;
+// Falling order by Batcher's odd-even merge sort.
+template <int N, typename K> __device__ __forceinline__ void sort_falling(K (&v)[N]) {
+#pragma unroll
+    for (int p = 1; p < N; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int j = k % p; j + k < N; j += 2 * k)
+#pragma unroll
+                for (int i = 0; i < k; ++i)
+                    if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                        const K a = v[i + j], b = v[i + j + k];
+                        v[i + j] = bigger(a, b);
+                        v[i + j + k] = smaller(a, b);
+                    }
+}
+// b where the mask is set, a elsewhere: written as a selection, array elements i and i + 1 become one element of a computed number.
+__device__ __forceinline__ unsigned merge(unsigned a, unsigned b, unsigned mask) { return (b & mask) | (a & ~mask); }
+__device__ __forceinline__ double merge(double a, double b, unsigned mask) {
+    return __hiloint2double(static_cast<int>(merge(static_cast<unsigned>(__double2hiint(a)), static_cast<unsigned>(__double2hiint(b)), mask)),
+                            static_cast<int>(merge(static_cast<unsigned>(__double2loint(a)), static_cast<unsigned>(__double2loint(b)), mask)));
+}
+// Lane j < top_k of the token's ends up with its choice j as a key.
+template <typename KEY, int LPT, int EPL>
+__device__ __forceinline__ typename KEY::type choose(typename KEY::type (&v)[EPL], int l, int top_k) {
+    typedef typename KEY::type K;
+    constexpr bool SORTED = EPL <= 16;
+    if constexpr (SORTED) sort_falling(v);
+    K chosen = KEY::NONE;
+    for (int j = 0; j < top_k; ++j) {
+        K best = v[0];
+        if constexpr (!SORTED) {
+#pragma unroll
+            for (int i = 1; i < EPL; ++i) best = bigger(best, v[i]);
+        }
+        const K most = lanes_max<LPT>(best);
+        if constexpr (SORTED) {
+            const unsigned mine = v[0] == most ? ~0u : 0u;
+#pragma unroll
+            for (int i = 0; i + 1 < EPL; ++i) v[i] = merge(v[i], v[i + 1], mine);
+            v[EPL - 1] = merge(v[EPL - 1], KEY::NONE, mine);
+        } else {
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) v[i] = v[i] == most ? KEY::NONE : v[i];
+        }
+        chosen = l == j ? most : chosen;
+    }
+    return chosen;
+}
+
+// Where the whole wave chooses for one token, which lane and which of its places hold a maximum is a matter of scalar instructions, and the keys need not hold the expert: float32 values in the
+// order of words, 0 for no expert.  Lane j < top_k ends up with its choice j (others are left as they were).
+__device__ __forceinline__ unsigned ordered(float v) {
+    const unsigned bits = __float_as_uint(v + 0.0f);                       // (-0 is as large as 0)
+    return v > -INFINITY ? bits ^ (static_cast<unsigned>(static_cast<int>(bits) >> 31) | 0x80000000u) : 0u;
+}
+__device__ __forceinline__ float from_ordered(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+template <int EPL>
+__device__ __forceinline__ void choose_wave(unsigned (&v)[EPL], int top_k, int shift, int per, int& chosen, unsigned& its) {
+    for (int j = 0; j < top_k; ++j) {
+        unsigned best = v[0];
+#pragma unroll
+        for (int i = 1; i < EPL; ++i) best = bigger(best, v[i]);
+        const unsigned most = static_cast<unsigned>(__builtin_amdgcn_readfirstlane(static_cast<int>(lanes_max<64>(best))));
+        if (most == 0) break;
+        uint64_t held[EPL], any = 0;
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
-            const double v = static_cast<double>(value[i]);
-            b = bigger(b, __builtin_fmin(a, v));
-            a = bigger(a, v);
+            held[i] = __ballot(v[i] == most);
+            any |= held[i];
         }
-        best_two<1, LPT>(a, b, group_lanes);
-        const double sum = c.group_best == 2 && b > NONE ? a + b : a;
-        int before = 0;
+        const int owner = __builtin_ctzll(any);
+        const uint64_t bit = uint64_t{1} << owner;
+        int place = 0;
+        bool open = true;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            const bool here = open && (held[i] & bit) != 0;
+            place = here ? i : place;
+            open = open && !here;
+            const bool gone = here && static_cast<int>(threadIdx.x & 63) == owner;
+            v[i] = gone ? 0u : v[i];
+        }
+        const bool mine = static_cast<int>(threadIdx.x & 63) == j;
+        chosen = mine ? (owner >> shift) * per + (owner & ((1 << shift) - 1)) * EPL + place : chosen;
+        its = mine ? most : its;
+    }
+}
+
+// The groups that stay: a group's place is the number of groups that come before it, those with more and those with as much and a lower number.  sum: of the lane's group.
+template <int LPT, typename V> __device__ __forceinline__ bool group_stays(const RouteCall& c, V sum, int lane, int group) {
+    int before = 0;
+    if constexpr (std::is_same<V, float>::value) {
+        const unsigned mine = ordered(sum);
+#pragma unroll 4
         for (int h = 0; h < c.n_groups; ++h) {
-            const int from = ((lane & ~(LPT - 1)) + h * group_lanes) * 4;
-            const double other = __hiloint2double(__builtin_amdgcn_ds_bpermute(from, __double2hiint(sum)), __builtin_amdgcn_ds_bpermute(from, __double2loint(sum)));
-            before += other > sum || (other == sum && h < group) ? 1 : 0;
+            const unsigned other = static_cast<unsigned>(lane_value<LPT>(static_cast<int>(mine), LPT == 64 ? h << c.group_shift : (lane & ~(LPT - 1)) + (h << c.group_shift)));
+            before += (h < group ? other >= mine : other > mine) ? 1 : 0;
         }
-        if (before >= c.top_groups)
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) value[i] = NONE;
-        else if (!c.bias)
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) value[i] = static_cast<V>(logit[i]);
+        return before < c.top_groups;
     }
+#pragma unroll 4
+    for (int h = 0; h < c.n_groups; ++h) {
+        const V other = lane_value<LPT>(sum, LPT == 64 ? h << c.group_shift : (lane & ~(LPT - 1)) + (h << c.group_shift));
+        before += other > sum || (other == sum && h < group) ? 1 : 0;
+    }
+    return before < c.top_groups;
+}
+template <int LPT, int EPL, typename V> __device__ __forceinline__ V group_sum(const RouteCall& c, const V (&value)[EPL]) {
+    V a = -INFINITY, b = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        b = bigger(b, smaller(a, value[i]));
+        a = bigger(a, value[i]);
+    }
+    best_two<1, LPT>(a, b, 1 << c.group_shift);
+    return c.group_best == 2 && b > static_cast<V>(-INFINITY) ? a + b : a;
+}
 
-    // lane j of the token's ends up with its choice j
+// exp(x) to 2^-31, in 64 bits so that nothing but the last rounding counts in float32: 2^n times the exponential's series up to the eighth power of |r| <= ln(2) / 2 (the ninth is 2e-10).
+__device__ __forceinline__ double exp64(double x) {
+    x = __builtin_fmin(__builtin_fmax(x, -800.0), 800.0);
+    const double n = __builtin_rint(x * 1.4426950408889634), r = __builtin_fma(n, -0.6931471805599453, x);
+    double p = 1.0 / 40320.0;
+    p = __builtin_fma(p, r, 1.0 / 5040.0);
+    p = __builtin_fma(p, r, 1.0 / 720.0);
+    p = __builtin_fma(p, r, 1.0 / 120.0);
+    p = __builtin_fma(p, r, 1.0 / 24.0);
+    p = __builtin_fma(p, r, 1.0 / 6.0);
+    p = __builtin_fma(p, r, 0.5);
+    p = __builtin_fma(p, r, 1.0);
+    p = __builtin_fma(p, r, 1.0);
+    return __builtin_ldexp(p, static_cast<int>(n));
+}
+// 1 / x for x of ordinary size, to about 2^-45: the reciprocal instruction and one step of Newton's
+__device__ __forceinline__ double over64(double x) {
+    const double r = __builtin_amdgcn_rcp(x);
+    return x > 0x1p1000 ? 0.0 : __builtin_fma(r, __builtin_fma(-x, r, 1.0), r);
+}
+
+// The choice in 64 bits.  Returns the expert and sets its logit in lane j.
+template <int LPT, int EPL>
+__device__ __forceinline__ int choose_exactly(const RouteCall& c, const float (&logit)[EPL], float top, int l, int lane, int group, int expert0, int mine, float& chosen_logit) {
+    constexpr double NONE = -INFINITY;
+    double value[EPL], all = 0.0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        value[i] = logit[i] == -INFINITY ? 0.0 : exp(c.sigmoid ? -static_cast<double>(logit[i]) : static_cast<double>(logit[i]) - static_cast<double>(top));
+        all += value[i];
+    }
+    if (!c.sigmoid) all = lanes_sum<LPT>(all);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        double v = c.sigmoid ? 1.0 / (1.0 + value[i]) : value[i] / all;
+        if (c.bias && i < mine) v += static_cast<double>(c.bias[expert0 + i]);
+        value[i] = logit[i] > -INFINITY && v > NONE ? v : NONE;            // (a bias of NaN or -infinity takes its expert out)
+    }
+    if (c.n_groups > 1) {
+        const bool stays = group_stays<LPT>(c, group_sum<LPT, EPL>(c, value), lane, group);
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) value[i] = !stays ? NONE : c.bias ? value[i] : static_cast<double>(logit[i]);
+    }
     int chosen = -1;
-    float chosen_logit = 0.f;
+    chosen_logit = 0.f;
     for (int j = 0; j < c.top_k; ++j) {
-        V best = value[0];
+        double best = value[0];
 #pragma unroll
         for (int i = 1; i < EPL; ++i) best = bigger(best, value[i]);
-        const V most = lanes_max<LPT>(best);
+        const double most = lanes_max<LPT>(best);
         const uint64_t held = __ballot(best == most && most > NONE);
         const unsigned seg = LPT == 64 ? 0 : static_cast<unsigned>(lane & ~(LPT - 1));
         const uint64_t here = LPT == 64 ? held : (held >> seg) & ((uint64_t{1} << (LPT & 63)) - 1);
@@ -184,60 +321,272 @@ route_kernel(RouteCall c) {
         const float x = __int_as_float(__builtin_amdgcn_ds_bpermute(from, __float_as_int(its)));
         if (l == j && here) { chosen = e; chosen_logit = x; }
     }
+    return chosen;
+}
+
+// The first `looked` lanes' experts, with their logits, in the order of their values in 64 bits.
+template <int LPT, int EPL>
+__device__ __forceinline__ void put_in_order(const RouteCall& c, const float (&logit)[EPL], float top, int l, int lane, int looked, float bias, int& chosen, float& chosen_logit) {
+    const double x = static_cast<double>(chosen_logit);
+    double v = exp(c.sigmoid ? -x : x - static_cast<double>(top));
+    if (c.sigmoid) {
+        v = 1.0 / (1.0 + v);
+    } else {
+        double all = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < EPL; ++i) {
+            float at = logit[0];
+#pragma unroll
+            for (int q = 1; q < EPL; ++q) at = i == q ? logit[q] : at;
+            all += at == -INFINITY ? 0.0 : exp(static_cast<double>(at) - static_cast<double>(top));
+        }
+        v /= lanes_sum<LPT>(all);
+    }
+    v = chosen < 0 ? -INFINITY : v + static_cast<double>(bias);
+    const int e = chosen < 0 ? 1024 + l : chosen;
+    int rank = 0;
+#pragma unroll 1
+    for (int j = 0; j < looked; ++j) {
+        const int from = LPT == 64 ? j : (lane & ~(LPT - 1)) + j;
+        const double other = lane_value<LPT>(v, from);
+        rank += other > v || (other == v && lane_value<LPT>(e, from) < e) ? 1 : 0;
+    }
+    const int to = ((lane & ~(LPT - 1)) + (l < looked ? rank : l)) * 4;
+    chosen = __builtin_amdgcn_ds_permute(to, chosen);
+    chosen_logit = __int_as_float(__builtin_amdgcn_ds_permute(to, __float_as_int(chosen_logit)));
+}
+
+// LPT lanes choose the experts of a token.  A group has LPT / (n_groups rounded up to a power of two) lanes of EPL experts each, in order, so that the lowest lane and then its lowest
+// place hold the lowest expert.
+// Without bias and groups the scores lie in the order of the logits (SCORED false).  With them the choice is that of values in 64 bits: in 32 bits the rounding of the exponential would decide
+// between experts that differ by less, and another order of the same operations would choose others.  It is made in 32 bits all the same, and made again in 64 where that cannot be sure: where
+// two values that follow each other in the choice, or the last group that stays and the first that does not, are closer than the errors of both.  (Equal values of equal logits and biases are.)
+template <typename T, int LPT, int EPL, bool SCORED>
+__global__ void __launch_bounds__(kThreads)
+route_kernel(RouteCall c) {
+    typedef typename std::conditional<!SCORED && sizeof(T) == 2, NarrowKey, WideKey>::type Key;
+    const int lane = threadIdx.x & 63, l = lane & (LPT - 1);
+    const int64_t token = (static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6)) * (64 / LPT) + lane / LPT;
+    if (token - lane / LPT >= c.n_tokens) return;                          // (the whole wave)
+    const bool there = token < c.n_tokens, routed = there && (!c.mask || c.mask[token] != 0);
+    const int group_lanes = SCORED ? 1 << c.group_shift : LPT, group = SCORED ? l >> c.group_shift : 0, per = SCORED ? c.per : c.n_experts;
+    const int first = (l & (group_lanes - 1)) * EPL, expert0 = group * per + first;      // of this lane
+    int mine = group < c.n_groups ? per - first : 0;                       // its experts
+    mine = mine < 0 ? 0 : (mine < EPL ? mine : EPL);
+
+    float logit[EPL];
+    const T* row = static_cast<const T*>(c.logits) + (routed ? token : 0) * c.n_experts;
+    if (c.whole) {
+        typedef T piece __attribute__((ext_vector_type(EPL * sizeof(T) > 16 ? 16 / sizeof(T) : EPL)));
+        constexpr int PE = sizeof(piece) / sizeof(T);
+        piece p[EPL / PE];
+        const bool any = group < c.n_groups;
+#pragma unroll
+        for (int i = 0; i < EPL / PE; ++i) p[i] = reinterpret_cast<const piece*>(row + (any ? expert0 : 0))[i];
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            T v;
+            if constexpr (PE == 1) v = reinterpret_cast<const T*>(p)[i]; else v = p[i / PE][i % PE];
+            logit[i] = any ? as_float<T>(v) : -INFINITY;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) logit[i] = i < mine ? as_float<T>(row[expert0 + i]) : -INFINITY;
+    }
+    float bias[SCORED ? EPL : 1];                                          // (requested with the logits)
+    if constexpr (SCORED) {
+        if (c.bias && c.whole) {
+            typedef float piece __attribute__((ext_vector_type(EPL > 4 ? 4 : EPL)));
+            constexpr int PE = sizeof(piece) / sizeof(float);
+#pragma unroll
+            for (int i = 0; i < EPL; i += PE) {
+                const piece p = *reinterpret_cast<const piece*>(c.bias + (group < c.n_groups ? expert0 : 0) + i);
+#pragma unroll
+                for (int e = 0; e < PE; ++e) bias[i + e] = reinterpret_cast<const float*>(&p)[e];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) bias[i] = c.bias && i < mine ? c.bias[expert0 + i] : 0.f;
+        }
+    }
+    // NaN is no score at all; what overflows counts as the largest value there is (NarrowKey: in its place, infinity)
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        if constexpr (std::is_same<Key, WideKey>::value) logit[i] = logit[i] < 3.402823466e38f ? logit[i] : logit[i] > 0.f ? 3.402823466e38f : -INFINITY;
+        else logit[i] = logit[i] > -INFINITY ? logit[i] : -INFINITY;
+    }
+
+    float top = 0.f;
+    double all = 0.0;                                                      // sum of the softmax's exponentials
+    if (!c.sigmoid && (SCORED || !c.renormalise)) {
+        top = logit[0];
+#pragma unroll
+        for (int i = 1; i < EPL; ++i) top = bigger(top, logit[i]);
+        top = lanes_max<LPT>(top);
+        top = __builtin_fminf(top, 3.402823466e38f);
+    }
+    typedef typename std::conditional<LPT == 64, unsigned, typename Key::type>::type K;
+    K key[EPL];
+    auto make_key = [](float v, int expert) { if constexpr (LPT == 64) return ordered(v); else return Key::make(v, expert); };
+    float value[EPL];
+    float thin = INFINITY;                                                 // the gap between the groups that stay and the others, less what it has to be at least
+    if constexpr (SCORED) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            value[i] = logit[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((c.sigmoid ? -logit[i] : logit[i] - top) * 1.4426950408889634f);
+            sum += value[i];
+        }
+        if (!c.sigmoid) sum = lanes_sum<LPT>(sum);
+        const float over = c.sigmoid ? 1.f : __builtin_amdgcn_rcpf(sum);
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            float v = c.sigmoid ? __builtin_amdgcn_rcpf(1.f + value[i]) : value[i] * over;
+            if (c.bias) v += bias[i];
+            value[i] = logit[i] > -INFINITY && v > -INFINITY ? v : -INFINITY;
+        }
+        bool stays = true;
+        if (c.n_groups > 1) {
+            const float s = group_sum<LPT, EPL>(c, value);
+            stays = group_stays<LPT>(c, s, lane, group);
+            if (c.top_groups < c.n_groups) {
+                const bool real = group < c.n_groups;
+                const float in = lanes_min<LPT>(real && stays ? s : INFINITY), out = lanes_max<LPT>(real && !stays ? s : -INFINITY);
+                // in = out = -infinity (groups without experts) is sure; so are infinite gaps
+                thin = in == -INFINITY || in - out == INFINITY ? INFINITY : in - out - 0x1p-20f * ((c.sigmoid ? 1.25f : 16.f) + 0.5f * (__builtin_fabsf(in) + __builtin_fabsf(out)));
+                thin = thin == thin ? thin : -1.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) {
+            value[i] = stays ? value[i] : -INFINITY;
+            key[i] = make_key(!stays ? -INFINITY : c.bias ? value[i] : logit[i], expert0 + i);
+        }
+    } else {
+        if (!c.sigmoid && !c.renormalise) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) sum += logit[i] == -INFINITY ? 0.f : expf(__builtin_fminf(logit[i], 3.402823466e38f) - top);
+            all = lanes_sum<LPT>(sum);
+        }
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) key[i] = make_key(logit[i], expert0 + i);
+    }
+
+    // lane j of the token's ends up with its choice j; where the choice has to be sure, the first two that are not chosen are looked at, too
+    const bool check = SCORED && c.bias != nullptr;
+    const int looked = check ? c.top_k + 2 : c.top_k;
+    int chosen = -1;
+    float chosen_logit = 0.f;
+    if constexpr (LPT == 64) {
+        unsigned its = 0;
+        choose_wave<EPL>(key, looked, SCORED ? c.group_shift : 6, per, chosen, its);
+        if (chosen >= 0) chosen_logit = from_ordered(its);
+    } else {
+        const K took = choose<Key, LPT, EPL>(key, l, looked);
+        if (took != Key::NONE) { chosen = Key::expert(took); chosen_logit = Key::value(took); }
+    }
+    if constexpr (SCORED) {
+        bool sure = thin > 0.f;
+        if (check) {
+            const float v = chosen < 0 ? -INFINITY : chosen_logit, b = chosen < 0 ? 0.f : c.bias[chosen];
+            chosen_logit = chosen < 0 ? 0.f : as_float<T>(row[chosen]);
+            const float next_v = __shfl_down(v, 1, LPT), next_b = __shfl_down(b, 1, LPT), next_x = __shfl_down(chosen_logit, 1, LPT), last_v = __shfl_down(v, 2, LPT);
+            const float least = (c.sigmoid ? 0x1p-21f : 0x1p-20f) * (1.f + __builtin_fabsf(v)) + (c.sigmoid ? 0.f : 0x1p-17f * (__builtin_fabsf(v - b) + __builtin_fabsf(next_v - next_b)));
+            const bool near = l < c.top_k && next_v > -INFINITY && !(v - next_v > least) && !(next_x == chosen_logit && next_b == b);
+            // the last choice and the second one behind it too near: there may be more of them (infinities of one sign: as near as can be)
+            const bool crowded = l == c.top_k - 1 && last_v > -INFINITY && !(v - last_v > least);
+            if (__ballot(crowded && routed)) {
+                const int from = LPT == 64 ? c.top_k - 1 : (lane & ~(LPT - 1)) + c.top_k - 1;
+                const float edge_v = lane_value<LPT>(v, from), edge_b = lane_value<LPT>(b, from), edge_x = lane_value<LPT>(chosen_logit, from), edge = lane_value<LPT>(least, from);
+                const bool look = lane_value<LPT>(crowded ? 1 : 0, from) != 0;
+#pragma unroll
+                for (int i = 0; i < EPL; ++i)
+                    if (look && i < mine && !(__builtin_fabsf(value[i] - edge_v) > edge) && value[i] > -INFINITY) sure = sure && logit[i] == edge_x && c.bias[expert0 + i] == edge_b;
+            }
+            if (__ballot(near && routed)) put_in_order<LPT, EPL>(c, logit, top, l, lane, looked, b, chosen, chosen_logit);
+            if (l >= c.top_k) chosen = -1;
+        }
+        chosen_logit = __builtin_fminf(chosen_logit, 3.402823466e38f);
+        // once for all tokens of the wave
+        if (__ballot(!sure && routed)) {
+            chosen = choose_exactly<LPT, EPL>(c, logit, top, l, lane, group, expert0, mine, chosen_logit);
+        }
+        if (!c.sigmoid && !c.renormalise) {
+            all = 0.0;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) all += logit[i] == -INFINITY ? 0.0 : exp(static_cast<double>(logit[i]) - static_cast<double>(top));
+            all = lanes_sum<LPT>(all);
+        }
+    }
     // Weights, in 64 bits: once per wave.  Renormalised softmax weights do not depend on the other experts, nor on how far below them the chosen ones lie.
+    chosen_logit = __builtin_fminf(chosen_logit, 3.402823466e38f);
     const bool has = routed && chosen >= 0;
     double w = 0.0;
     if (c.sigmoid) {
-        if (has) w = 1.0 / (1.0 + exp(-static_cast<double>(chosen_logit)));
+        w = has ? over64(1.0 + exp64(-static_cast<double>(chosen_logit))) : 0.0;
     } else {
         const float from = c.renormalise ? lanes_max<LPT>(has ? chosen_logit : -INFINITY) : top;
-        if (has) w = exp(static_cast<double>(chosen_logit) - static_cast<double>(from));
-        if (has && !c.renormalise) w /= all;
+        w = has ? exp64(static_cast<double>(chosen_logit) - static_cast<double>(from)) : 0.0;
     }
-    if (c.renormalise) {
-        const double sum = lanes_sum<LPT>(w);
-        w = sum > 0.0 ? w / sum : 0.0;
-    }
+    if (c.renormalise) all = lanes_sum<LPT>(w);
+    if (c.renormalise || !c.sigmoid) w = all > 0.0 ? w * over64(all) : 0.0;
     if (there && l < c.top_k) {
         c.expert[token * c.top_k + l] = has ? chosen : -1;
         c.weight[token * c.top_k + l] = has ? static_cast<float>(w * static_cast<double>(c.scale)) : 0.f;
     }
 }
 
+// experts of a lane where LPT lanes share a token
+int experts_per_lane(RouteCall& c, int lpt) {
+    c.per = c.n_experts / c.n_groups;
+    c.group_shift = lpt == 16 ? 4 : 6;
+    for (int g = 1; g < c.n_groups; g *= 2) --c.group_shift;
+    return (c.per + (1 << c.group_shift) - 1) >> c.group_shift;
+}
 template <typename T, int LPT, int EPL>
-int launch_route(regione_ctx* ctx, RouteCall& c, bool exact) {
-    c.group_lanes = LPT;
-    for (int g = 1; g < c.n_groups; g *= 2) c.group_lanes /= 2;
-    c.whole = c.n_experts / c.n_groups == c.group_lanes * EPL;
+int launch_route(regione_ctx* ctx, RouteCall& c, bool scored) {
+    c.whole = c.per == EPL << c.group_shift && rg_aligned16(c.bias);
     const int64_t tokens_per = (kThreads / 64) * (64 / LPT), blocks = (c.n_tokens + tokens_per - 1) / tokens_per;
-    if (exact) hipLaunchKernelGGL((route_kernel<T, LPT, EPL, true>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, ctx->stream, c);
+    if (scored) hipLaunchKernelGGL((route_kernel<T, LPT, EPL, true>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, ctx->stream, c);
     else hipLaunchKernelGGL((route_kernel<T, LPT, EPL, false>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, ctx->stream, c);
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }
 template <typename T>
-int launch_route(regione_ctx* ctx, RouteCall& c, bool exact) {
-    int lanes = 64;
-    for (int g = 1; g < c.n_groups; g *= 2) lanes /= 2;
-    const int need = (c.n_experts / c.n_groups + lanes - 1) / lanes;
-    if (need <= 1) return launch_route<T, 64, 1>(ctx, c, exact);
-    if (need <= 2) return launch_route<T, 64, 2>(ctx, c, exact);
-    if (need <= 4) return launch_route<T, 64, 4>(ctx, c, exact);
-    if (need <= 8) return launch_route<T, 64, 8>(ctx, c, exact);
-    if (need <= 16) return launch_route<T, 64, 16>(ctx, c, exact);
-    return launch_route<T, 64, 32>(ctx, c, exact);
+int launch_route(regione_ctx* ctx, RouteCall& c, bool scored) {
+    // (two lanes more than choices)
+    if (c.n_tokens >= kRouteShared && c.top_k <= 14 && c.n_groups <= 16) {
+        const int need = experts_per_lane(c, 16);
+        if (need <= 4) return launch_route<T, 16, 4>(ctx, c, scored);
+        if (need <= 8) return launch_route<T, 16, 8>(ctx, c, scored);
+        if (need <= 16) return launch_route<T, 16, 16>(ctx, c, scored);
+    }
+    const int need = experts_per_lane(c, 64);
+    if (need <= 1) return launch_route<T, 64, 1>(ctx, c, scored);
+    if (need <= 2) return launch_route<T, 64, 2>(ctx, c, scored);
+    if (need <= 4) return launch_route<T, 64, 4>(ctx, c, scored);
+    if (need <= 8) return launch_route<T, 64, 8>(ctx, c, scored);
+    if (need <= 16) return launch_route<T, 64, 16>(ctx, c, scored);
+    return launch_route<T, 64, 32>(ctx, c, scored);
 }
 
 // ---- the sort by expert
 
-// A stable counting sort.  The pairs are cut into chunks of whole rounds of kRound; every workgroup counts its chunk, and a second launch places it behind the chunks before: the waves of
-// a workgroup own consecutive parts of the chunk, so that a pair's place is its expert's first row + the expert's pairs of earlier chunks, of earlier waves, and of earlier pairs of its wave.
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostChunks = 256, kSortLeast = 512;      // kSortLeast: pairs per wave of a chunk at least, where there are several
+// A stable counting sort.  The pairs are cut into chunks of whole parts of 8192; every workgroup counts its chunk, and a second launch places it behind the chunks before: a wave owns 512
+// consecutive pairs of a part, which stay in its registers between their counting and their placing, so that a pair's place is its expert's first row + the expert's pairs of
+// earlier chunks, of earlier parts, of earlier waves, and of earlier pairs of its wave.  Up to 8192 pairs are one chunk and one launch.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostChunks = 256, kPairsAhead = 8, kSortPart = kSortThreads * kPairsAhead;
 
-__device__ __forceinline__ int pair_expert(const int32_t* expert, int64_t at, int64_t end, int n_experts) {
-    if (at >= end) return -1;
-    const int e = expert[at];
-    return e >= 0 && e < n_experts ? e : -1;
+// pair number q of a lane: the wave's pairs 64 q + lane
+__device__ __forceinline__ void load_pairs(const int32_t* expert, int64_t wave0, int64_t end, int n_experts, int (&id)[kPairsAhead]) {
+#pragma unroll
+    for (int q = 0; q < kPairsAhead; ++q) {
+        const int64_t at = wave0 + 64 * q + (threadIdx.x & 63);
+        id[q] = at < end ? expert[at] : -1;
+    }
+#pragma unroll
+    for (int q = 0; q < kPairsAhead; ++q) id[q] = id[q] >= 0 && id[q] < n_experts ? id[q] : -1;
 }
 __global__ void __launch_bounds__(kSortThreads)
 count_pairs_kernel(const int32_t* __restrict__ expert, int64_t n, int64_t per_chunk, int n_experts, int32_t* __restrict__ counts) {
@@ -245,82 +594,106 @@ count_pairs_kernel(const int32_t* __restrict__ expert, int64_t n, int64_t per_ch
     for (int e = threadIdx.x; e < n_experts; e += kSortThreads) count[e] = 0;
     __syncthreads();
     const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_chunk, end = begin + per_chunk < n ? begin + per_chunk : n;
-    for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads) {
-        const int e = pair_expert(expert, i, end, n_experts);
-        if (e >= 0) atomicAdd(&count[e], 1);
+    for (int64_t part = begin; part < end; part += kSortPart) {
+        int id[kPairsAhead];
+        load_pairs(expert, part + (threadIdx.x >> 6) * (64 * kPairsAhead), end, n_experts, id);
+#pragma unroll
+        for (int q = 0; q < kPairsAhead; ++q)
+            if (id[q] >= 0) atomicAdd(&count[id[q]], 1);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < n_experts; e += kSortThreads) counts[static_cast<int64_t>(blockIdx.x) * n_experts + e] = count[e];
 }
-// counts: [chunks][n_experts], or null where there is one chunk
+// counts: [chunks][n_experts], or null where there is one chunk.  A thread per expert adds things up; the sums over the chunks are shared by all threads.
 __global__ void __launch_bounds__(kSortThreads)
 place_pairs_kernel(const int32_t* __restrict__ expert, int64_t n, int64_t per_chunk, int n_experts, int bits, int top_k, const int32_t* __restrict__ counts,
                    int32_t* __restrict__ offsets, int32_t* __restrict__ row_token, int32_t* __restrict__ slot) {
-    extern __shared__ int32_t lds[];                                       // [kSortWaves][n_experts], then [kSortWaves]
+    extern __shared__ int32_t lds[];                                       // [kSortWaves][n_experts], then [kSortWaves]; before that the threads' sums over the chunks
     int32_t* const sums = lds + kSortWaves * n_experts;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = threadIdx.x;
     const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_chunk, end = begin + per_chunk < n ? begin + per_chunk : n;
-    const int64_t per_wave = (per_chunk / kSortWaves + 63) / 64 * 64;
-    const int64_t w0 = begin + wave * per_wave, w1 = w0 + per_wave < end ? w0 + per_wave : end;
-    for (int i = threadIdx.x; i < kSortWaves * n_experts; i += kSortThreads) lds[i] = 0;
-    __syncthreads();
-    for (int64_t i = w0 + lane; i < w1; i += 64) {
-        const int e = pair_expert(expert, i, w1, n_experts);
-        if (e >= 0) atomicAdd(&lds[wave * n_experts + e], 1);
+    int id[kPairsAhead];
+    load_pairs(expert, begin + wave * (64 * kPairsAhead), end, n_experts, id);
+
+    int before = 0, all = 0;                                               // this thread's expert's pairs: of the chunks before, and all
+    if (counts) {
+        const int shares = kSortThreads / n_experts, mine = e / n_experts, chunks = static_cast<int>(gridDim.x);
+        if (mine < shares) {
+            const int32_t* const at = counts + (e - mine * n_experts);
+#pragma unroll 8
+            for (int c = mine; c < chunks; c += shares) {
+                const int v = at[static_cast<int64_t>(c) * n_experts];
+                before += c < static_cast<int>(blockIdx.x) ? v : 0;
+                all += v;
+            }
+            lds[e] = before;
+            lds[kSortThreads + e] = all;
+        }
+        __syncthreads();
+        before = all = 0;
+        if (e < n_experts)
+            for (int t = e; t < shares * n_experts; t += n_experts) {
+                before += lds[t];
+                all += lds[kSortThreads + t];
+            }
+        __syncthreads();
     }
-    // this thread's expert: pairs of the chunks before, and all
-    const int e = threadIdx.x;
-    int before = 0, all = 0;
-    if (counts && e < n_experts)
-        for (unsigned c = 0; c < gridDim.x; ++c) {
-            const int v = counts[static_cast<int64_t>(c) * n_experts + e];
-            before += c < blockIdx.x ? v : 0;
-            all += v;
+    int next = 0;                                                          // where this thread's expert's next pair goes
+    for (int64_t part = begin; part < end || part == begin; part += kSortPart) {
+        if (part != begin) load_pairs(expert, part + wave * (64 * kPairsAhead), end, n_experts, id);
+        for (int i = threadIdx.x; i < kSortWaves * n_experts; i += kSortThreads) lds[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kPairsAhead; ++q)
+            if (id[q] >= 0) atomicAdd(&lds[wave * n_experts + id[q]], 1);
+        __syncthreads();
+        if (part == begin) {
+            if (!counts && e < n_experts) for (int w = 0; w < kSortWaves; ++w) all += lds[w * n_experts + e];
+            int upto = all;                                                // inclusive sums over the experts
+            for (int d = 1; d < 64; d *= 2) {
+                const int v = __shfl_up(upto, d);
+                upto += lane >= d ? v : 0;
+            }
+            if (lane == 63) sums[wave] = upto;
+            __syncthreads();
+            for (int w = 0; w < wave; ++w) upto += sums[w];
+            next = upto - all + before;
+            if (blockIdx.x == 0 && e < n_experts) {
+                offsets[e + 1] = upto;
+                if (e == 0) offsets[0] = 0;
+            }
         }
-    __syncthreads();
-    if (!counts && e < n_experts) for (int w = 0; w < kSortWaves; ++w) all += lds[w * n_experts + e];
-    int upto = all;                                                        // inclusive sums over the experts
-    for (int d = 1; d < 64; d *= 2) {
-        const int v = __shfl_up(upto, d);
-        upto += lane >= d ? v : 0;
-    }
-    if (lane == 63) sums[wave] = upto;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) upto += sums[w];
-    if (e < n_experts) {
-        if (blockIdx.x == 0) {
-            offsets[e + 1] = upto;
-            if (e == 0) offsets[0] = 0;
-        }
-        int at = upto - all + before;
-        for (int w = 0; w < kSortWaves; ++w) {
-            const int v = lds[w * n_experts + e];
-            lds[w * n_experts + e] = at;
-            at += v;
-        }
-    }
-    __syncthreads();
-    for (int64_t i0 = w0; i0 < w1; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const int id = pair_expert(expert, i, w1, n_experts);
-        uint64_t same = __ballot(id >= 0);                                 // lanes with this lane's expert
-        for (int b = 0; b < bits; ++b) {
-            const bool set = (id >> b) & 1;
-            const uint64_t with = __ballot(set);
-            same &= set ? with : ~with;
-        }
-        const int rank = __builtin_popcountll(same & ((uint64_t{1} << lane) - 1));
-        if (id >= 0) {
-            volatile int32_t* const next = &lds[wave * n_experts + id];           // (the other lanes' doing)
-            const int place = *next + rank;
+        if (e < n_experts)
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                const int v = lds[w * n_experts + e];
+                lds[w * n_experts + e] = next;
+                next += v;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kPairsAhead; ++q) {
+            const unsigned i = static_cast<unsigned>(part) + wave * (64 * kPairsAhead) + 64 * q + lane;
+            uint64_t same = __ballot(id[q] >= 0);                          // lanes with this lane's expert
+            for (int b = 0; b < bits; ++b) {
+                const bool set = (id[q] >> b) & 1;
+                const uint64_t with = __ballot(set);
+                same &= set ? with : ~with;
+            }
+            const int rank = __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(same >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(same), 0));
+            if (id[q] >= 0) {
+                volatile int32_t* const to = &lds[wave * n_experts + id[q]];      // (the other lanes change it)
+                const int place = *to + rank;
+                __builtin_amdgcn_wave_barrier();
+                if (rank == 0) *to = place + __builtin_popcountll(same);
+                slot[i] = place;
+                row_token[place] = static_cast<int32_t>(i / static_cast<unsigned>(top_k));
+            } else if (i < end) {
+                slot[i] = -1;
+            }
             __builtin_amdgcn_wave_barrier();
-            if (rank == 0) *next = place + __builtin_popcountll(same);
-            slot[i] = place;
-            row_token[place] = static_cast<int32_t>(i / top_k);
-        } else if (i < w1) {
-            slot[i] = -1;
         }
-        __builtin_amdgcn_wave_barrier();
+        __syncthreads();
     }
 }
 
@@ -431,10 +804,10 @@ extern "C" int regione_expert_route(regione_ctx* ctx, const void* logits, int32_
     if (n_tokens == 0) return REGIONE_OK;
     if (!logits || !expert || !weight) RG_FAIL(REGIONE_ERR_INVALID_ARG, "expert_route: null tensor");
     if (!rg_aligned16(logits)) RG_FAIL(REGIONE_ERR_INVALID_ARG, "expert_route: logits must be 16-byte aligned");
-    RouteCall c = {logits, bias_opt, mask_opt, expert, weight, n_tokens, n_experts, n_groups, top_groups, group_best, top_k, 0, score == REGIONE_SCORE_SIGMOID, renormalise != 0, 0, scale};
-    const bool exact = bias_opt || n_groups > 1;
+    RouteCall c = {logits, bias_opt, mask_opt, expert, weight, n_tokens, n_experts, n_groups, top_groups, group_best, top_k, 0, 0, score == REGIONE_SCORE_SIGMOID, renormalise != 0, 0, scale};
+    const bool scored = bias_opt || n_groups > 1;
     ProfScope prof(ctx, REGIONE_PROF_ROWS);
-    return dtype == REGIONE_FP32 ? launch_route<float>(ctx, c, exact) : launch_route<bf16_t>(ctx, c, exact);
+    return dtype == REGIONE_FP32 ? launch_route<float>(ctx, c, scored) : launch_route<bf16_t>(ctx, c, scored);
 }
 
 extern "C" int regione_expert_slots(regione_ctx* ctx, const int32_t* expert, int64_t n_tokens, int32_t top_k, int32_t n_experts, int32_t* group_offsets, int32_t* row_token, int32_t* slot) {
@@ -444,10 +817,7 @@ extern "C" int regione_expert_slots(regione_ctx* ctx, const int32_t* expert, int
         RG_FAIL(REGIONE_ERR_UNSUPPORTED, "expert_slots: %lld x %d pairs (at most 2^24, %d per token), %d experts (at most %d)", (long long)n_tokens, top_k, kMostChosen, n_experts, kMostExperts);
     if (!group_offsets || (n_tokens > 0 && (!expert || !row_token || !slot))) RG_FAIL(REGIONE_ERR_INVALID_ARG, "expert_slots: null tensor");
     const int64_t n = n_tokens * top_k;
-    int64_t chunks = (n + kSortWaves * kSortLeast - 1) / (kSortWaves * kSortLeast);
-    chunks = chunks < 1 ? 1 : (chunks < kMostChunks ? chunks : kMostChunks);
-    const int64_t round = kSortThreads, per_chunk = ((n + chunks - 1) / chunks + round - 1) / round * round;
-    chunks = n > 0 ? (n + per_chunk - 1) / per_chunk : 1;
+    const int64_t parts = (n + kSortPart - 1) / kSortPart, per_chunk = (parts + kMostChunks - 1) / kMostChunks * kSortPart, chunks = n > kSortPart ? (n + per_chunk - 1) / per_chunk : 1;
     if (chunks > 1 && static_cast<size_t>(chunks) * n_experts * sizeof(int32_t) > ctx->gemm_part_bytes)
         RG_FAIL(REGIONE_ERR_WORKSPACE, "expert_slots: %lld pairs need more workspace than the context has", (long long)n);
     int bits = 0;
@@ -458,7 +828,8 @@ extern "C" int regione_expert_slots(regione_ctx* ctx, const int32_t* expert, int
         hipLaunchKernelGGL(count_pairs_kernel, dim3(static_cast<unsigned>(chunks)), dim3(kSortThreads), 0, ctx->stream, expert, n, per_chunk, n_experts, counts);
         RG_LAUNCH_CHECK();
     }
-    const size_t lds = (static_cast<size_t>(kSortWaves) * n_experts + kSortWaves) * sizeof(int32_t);
+    size_t lds = (static_cast<size_t>(kSortWaves) * n_experts + kSortWaves) * sizeof(int32_t);
+    if (counts && lds < 2 * kSortThreads * sizeof(int32_t)) lds = 2 * kSortThreads * sizeof(int32_t);
     static std::atomic<uint64_t> granted{0};
     if (lds > 65536)
         if (int rc = rg_grant_lds(ctx, reinterpret_cast<const void*>(place_pairs_kernel), granted, (static_cast<size_t>(kSortWaves) * kMostExperts + kSortWaves) * sizeof(int32_t))) return rc;
