@@ -573,38 +573,43 @@ int launch_route(regione_ctx* ctx, RouteCall& c, bool scored) {
 
 // ---- the sort by expert
 
-// A stable counting sort.  The pairs are cut into chunks of whole parts of 8192; every workgroup counts its chunk, and a second launch places it behind the chunks before: a wave owns 512
-// consecutive pairs of a part, which stay in its registers between their counting and their placing, so that a pair's place is its expert's first row + the expert's pairs of
-// earlier chunks, of earlier parts, of earlier waves, and of earlier pairs of its wave.  Up to 8192 pairs are one chunk and one launch.
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostChunks = 256, kPairsAhead = 8, kSortPart = kSortThreads * kPairsAhead;
+// A stable counting sort.  The pairs are cut into chunks of whole parts of 1024 * AHEAD; every workgroup counts its chunk, and a second launch places it behind the chunks before: a wave owns
+// 64 * AHEAD consecutive pairs of a part, which stay in its registers between their counting and their placing, so that a pair's place is its expert's first row + the expert's pairs of
+// earlier chunks, of earlier parts, of earlier waves, and of earlier pairs of its wave.
+// Latency throughout: a few trips to memory, and a chain of LDS accesses per 64 pairs of a wave.  us, AHEAD 2 / 4 / 8 (one launch where a part holds all pairs, else two): 72 pairs of 16
+// experts 3.7 / 4.3 / 5.8, 4096 of 128 7.8 / 6.3 / 7.9, 8192 of 128 7.9 / 9.5 / 9.2, 65536 of 128 9.0 / 10.2 / 14.0, 524288 of 128 11.1 / 11.6 / 15.0, of 256 13.3 / 12.5 / 15.3.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kMostChunks = 256;
 
 // pair number q of a lane: the wave's pairs 64 q + lane
-__device__ __forceinline__ void load_pairs(const int32_t* expert, int64_t wave0, int64_t end, int n_experts, int (&id)[kPairsAhead]) {
+template <int AHEAD>
+__device__ __forceinline__ void load_pairs(const int32_t* expert, int64_t wave0, int64_t end, int n_experts, int (&id)[AHEAD]) {
 #pragma unroll
-    for (int q = 0; q < kPairsAhead; ++q) {
+    for (int q = 0; q < AHEAD; ++q) {
         const int64_t at = wave0 + 64 * q + (threadIdx.x & 63);
         id[q] = at < end ? expert[at] : -1;
     }
 #pragma unroll
-    for (int q = 0; q < kPairsAhead; ++q) id[q] = id[q] >= 0 && id[q] < n_experts ? id[q] : -1;
+    for (int q = 0; q < AHEAD; ++q) id[q] = id[q] >= 0 && id[q] < n_experts ? id[q] : -1;
 }
+template <int AHEAD>
 __global__ void __launch_bounds__(kSortThreads)
 count_pairs_kernel(const int32_t* __restrict__ expert, int64_t n, int64_t per_chunk, int n_experts, int32_t* __restrict__ counts) {
     __shared__ int32_t count[kMostExperts];
     for (int e = threadIdx.x; e < n_experts; e += kSortThreads) count[e] = 0;
     __syncthreads();
     const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_chunk, end = begin + per_chunk < n ? begin + per_chunk : n;
-    for (int64_t part = begin; part < end; part += kSortPart) {
-        int id[kPairsAhead];
-        load_pairs(expert, part + (threadIdx.x >> 6) * (64 * kPairsAhead), end, n_experts, id);
+    for (int64_t part = begin; part < end; part += kSortThreads * AHEAD) {
+        int id[AHEAD];
+        load_pairs(expert, part + (threadIdx.x >> 6) * (64 * AHEAD), end, n_experts, id);
 #pragma unroll
-        for (int q = 0; q < kPairsAhead; ++q)
+        for (int q = 0; q < AHEAD; ++q)
             if (id[q] >= 0) atomicAdd(&count[id[q]], 1);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < n_experts; e += kSortThreads) counts[static_cast<int64_t>(blockIdx.x) * n_experts + e] = count[e];
 }
 // counts: [chunks][n_experts], or null where there is one chunk.  A thread per expert adds things up; the sums over the chunks are shared by all threads.
+template <int AHEAD>
 __global__ void __launch_bounds__(kSortThreads)
 place_pairs_kernel(const int32_t* __restrict__ expert, int64_t n, int64_t per_chunk, int n_experts, int bits, int top_k, const int32_t* __restrict__ counts,
                    int32_t* __restrict__ offsets, int32_t* __restrict__ row_token, int32_t* __restrict__ slot) {
@@ -612,8 +617,8 @@ place_pairs_kernel(const int32_t* __restrict__ expert, int64_t n, int64_t per_ch
     int32_t* const sums = lds + kSortWaves * n_experts;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = threadIdx.x;
     const int64_t begin = static_cast<int64_t>(blockIdx.x) * per_chunk, end = begin + per_chunk < n ? begin + per_chunk : n;
-    int id[kPairsAhead];
-    load_pairs(expert, begin + wave * (64 * kPairsAhead), end, n_experts, id);
+    int id[AHEAD];
+    load_pairs(expert, begin + wave * (64 * AHEAD), end, n_experts, id);
 
     int before = 0, all = 0;                                               // this thread's expert's pairs: of the chunks before, and all
     if (counts) {
@@ -639,12 +644,12 @@ place_pairs_kernel(const int32_t* __restrict__ expert, int64_t n, int64_t per_ch
         __syncthreads();
     }
     int next = 0;                                                          // where this thread's expert's next pair goes
-    for (int64_t part = begin; part < end || part == begin; part += kSortPart) {
-        if (part != begin) load_pairs(expert, part + wave * (64 * kPairsAhead), end, n_experts, id);
+    for (int64_t part = begin; part < end || part == begin; part += kSortThreads * AHEAD) {
+        if (part != begin) load_pairs(expert, part + wave * (64 * AHEAD), end, n_experts, id);
         for (int i = threadIdx.x; i < kSortWaves * n_experts; i += kSortThreads) lds[i] = 0;
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < kPairsAhead; ++q)
+        for (int q = 0; q < AHEAD; ++q)
             if (id[q] >= 0) atomicAdd(&lds[wave * n_experts + id[q]], 1);
         __syncthreads();
         if (part == begin) {
@@ -672,8 +677,8 @@ place_pairs_kernel(const int32_t* __restrict__ expert, int64_t n, int64_t per_ch
             }
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < kPairsAhead; ++q) {
-            const unsigned i = static_cast<unsigned>(part) + wave * (64 * kPairsAhead) + 64 * q + lane;
+        for (int q = 0; q < AHEAD; ++q) {
+            const unsigned i = static_cast<unsigned>(part) + wave * (64 * AHEAD) + 64 * q + lane;
             uint64_t same = __ballot(id[q] >= 0);                          // lanes with this lane's expert
             for (int b = 0; b < bits; ++b) {
                 const bool set = (id[q] >> b) & 1;
@@ -787,6 +792,29 @@ int launch_combine(regione_ctx* ctx, const void* rows, int64_t n_rows, const int
     return launch_combine<TR, TO, 1>(ctx, rows, n_rows, slot, weight, base, n_tokens, top_k, cols, out);
 }
 
+template <int AHEAD>
+int launch_sort(regione_ctx* ctx, const int32_t* expert, int64_t n, int n_experts, int top_k, int32_t* offsets, int32_t* row_token, int32_t* slot) {
+    constexpr int64_t PART = kSortThreads * AHEAD;
+    const int64_t parts = (n + PART - 1) / PART, per_chunk = (parts + kMostChunks - 1) / kMostChunks * PART, chunks = n > PART ? (n + per_chunk - 1) / per_chunk : 1;
+    if (chunks > 1 && static_cast<size_t>(chunks) * n_experts * sizeof(int32_t) > ctx->gemm_part_bytes)
+        RG_FAIL(REGIONE_ERR_WORKSPACE, "expert_slots: %lld pairs need more workspace than the context has", (long long)n);
+    int bits = 0;
+    while ((1 << bits) < n_experts) ++bits;
+    int32_t* counts = chunks > 1 ? reinterpret_cast<int32_t*>(ctx->gemm_part) : nullptr;
+    if (counts) {
+        hipLaunchKernelGGL((count_pairs_kernel<AHEAD>), dim3(static_cast<unsigned>(chunks)), dim3(kSortThreads), 0, ctx->stream, expert, n, per_chunk, n_experts, counts);
+        RG_LAUNCH_CHECK();
+    }
+    size_t lds = (static_cast<size_t>(kSortWaves) * n_experts + kSortWaves) * sizeof(int32_t);
+    if (counts && lds < 2 * kSortThreads * sizeof(int32_t)) lds = 2 * kSortThreads * sizeof(int32_t);
+    static std::atomic<uint64_t> granted{0};
+    if (lds > 65536)
+        if (int rc = rg_grant_lds(ctx, reinterpret_cast<const void*>(place_pairs_kernel<AHEAD>), granted, (static_cast<size_t>(kSortWaves) * kMostExperts + kSortWaves) * sizeof(int32_t))) return rc;
+    hipLaunchKernelGGL((place_pairs_kernel<AHEAD>), dim3(static_cast<unsigned>(chunks)), dim3(kSortThreads), lds, ctx->stream, expert, n, per_chunk, n_experts, bits, top_k, counts, offsets, row_token, slot);
+    RG_LAUNCH_CHECK();
+    return REGIONE_OK;
+}
+
 }  // namespace
 
 extern "C" int regione_expert_route(regione_ctx* ctx, const void* logits, int32_t dtype, const float* bias_opt, const uint8_t* mask_opt, int64_t n_tokens, int32_t n_experts, int32_t score,
@@ -817,25 +845,9 @@ extern "C" int regione_expert_slots(regione_ctx* ctx, const int32_t* expert, int
         RG_FAIL(REGIONE_ERR_UNSUPPORTED, "expert_slots: %lld x %d pairs (at most 2^24, %d per token), %d experts (at most %d)", (long long)n_tokens, top_k, kMostChosen, n_experts, kMostExperts);
     if (!group_offsets || (n_tokens > 0 && (!expert || !row_token || !slot))) RG_FAIL(REGIONE_ERR_INVALID_ARG, "expert_slots: null tensor");
     const int64_t n = n_tokens * top_k;
-    const int64_t parts = (n + kSortPart - 1) / kSortPart, per_chunk = (parts + kMostChunks - 1) / kMostChunks * kSortPart, chunks = n > kSortPart ? (n + per_chunk - 1) / per_chunk : 1;
-    if (chunks > 1 && static_cast<size_t>(chunks) * n_experts * sizeof(int32_t) > ctx->gemm_part_bytes)
-        RG_FAIL(REGIONE_ERR_WORKSPACE, "expert_slots: %lld pairs need more workspace than the context has", (long long)n);
-    int bits = 0;
-    while ((1 << bits) < n_experts) ++bits;
     ProfScope prof(ctx, REGIONE_PROF_ROWS);
-    int32_t* counts = chunks > 1 ? reinterpret_cast<int32_t*>(ctx->gemm_part) : nullptr;
-    if (counts) {
-        hipLaunchKernelGGL(count_pairs_kernel, dim3(static_cast<unsigned>(chunks)), dim3(kSortThreads), 0, ctx->stream, expert, n, per_chunk, n_experts, counts);
-        RG_LAUNCH_CHECK();
-    }
-    size_t lds = (static_cast<size_t>(kSortWaves) * n_experts + kSortWaves) * sizeof(int32_t);
-    if (counts && lds < 2 * kSortThreads * sizeof(int32_t)) lds = 2 * kSortThreads * sizeof(int32_t);
-    static std::atomic<uint64_t> granted{0};
-    if (lds > 65536)
-        if (int rc = rg_grant_lds(ctx, reinterpret_cast<const void*>(place_pairs_kernel), granted, (static_cast<size_t>(kSortWaves) * kMostExperts + kSortWaves) * sizeof(int32_t))) return rc;
-    hipLaunchKernelGGL(place_pairs_kernel, dim3(static_cast<unsigned>(chunks)), dim3(kSortThreads), lds, ctx->stream, expert, n, per_chunk, n_experts, bits, top_k, counts, group_offsets, row_token, slot);
-    RG_LAUNCH_CHECK();
-    return REGIONE_OK;
+    if (n <= 2048 || (n > 4096 && n <= 262144)) return launch_sort<2>(ctx, expert, n, n_experts, top_k, group_offsets, row_token, slot);
+    return launch_sort<4>(ctx, expert, n, n_experts, top_k, group_offsets, row_token, slot);
 }
 
 extern "C" int regione_expert_combine(regione_ctx* ctx, const void* rows, int32_t rows_dtype, int64_t n_rows, const int32_t* slot, const float* weight_opt, const void* base_opt,
