@@ -5,17 +5,22 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kNoAdapter = 0x7fffffff;
 constexpr int kMostRank = 256, kMostSel = 32, kMostAdapters = 1 << 16;
-constexpr size_t kTermBytes = size_t{32} << 20;              // of the inner products of the rows that go through at a time
+constexpr int kLeastChunk = 1024;                        // rows of a pass below which tiles leave their work to the kernel of 16 rows
+constexpr size_t kTermBytes = size_t{32} << 20;          // of the inner products of the rows that go through at a time
 
-// A packed adapter: A in fragments of 16 ranks x 32 inputs, 64 lanes x 8 values, lane l holding A[16 * (block) + l % 16][32 * step + 8 * (l / 16) .. +8]; behind it B as regione_pack_weight
+// A packed adapter: behind A and B a bit per column of B that holds a value that is not finite (zero in B), 32 to a word, a word that is not zero if there is one, and zeros up to 16 bytes.
+// A in fragments of 16 ranks x 32 inputs, 64 lanes x 8 values, lane l holding A[16 * (block) + l % 16][32 * step + 8 * (l / 16) .. +8]; behind it B as regione_pack_weight
 // lays out a weight [n, rank rounded up to 16].
 __host__ __device__ __forceinline__ int64_t a_elems(int k, int blocks) { return static_cast<int64_t>(blocks) * 16 * k; }
-__host__ __device__ __forceinline__ int64_t adapter_elems(int n, int k, int blocks) { return a_elems(k, blocks) + (static_cast<int64_t>(n) + 31) / 32 * 32 * blocks * 16; }
+__host__ __device__ __forceinline__ int64_t b_elems(int n, int blocks) { return (static_cast<int64_t>(n) + 31) / 32 * 32 * blocks * 16; }
+__host__ __device__ __forceinline__ int64_t bad_words(int n) { return ((static_cast<int64_t>(n) + 31) / 32 + 1 + 3) / 4 * 4; }
+__host__ __device__ __forceinline__ int64_t adapter_elems(int n, int k, int blocks) { return a_elems(k, blocks) + b_elems(n, blocks) + 2 * bad_words(n); }
 
 __global__ void __launch_bounds__(kThreads)
 pack_adapter_kernel(const bf16_t* __restrict__ a, const bf16_t* __restrict__ b, int n, int k, int rank, int blocks, bf16_t* __restrict__ packed) {
-    const int64_t a_count = a_elems(k, blocks), count = adapter_elems(n, k, blocks), stride = static_cast<int64_t>(gridDim.x) * kThreads;
+    const int64_t a_count = a_elems(k, blocks), b_end = a_count + b_elems(n, blocks), count = adapter_elems(n, k, blocks), stride = static_cast<int64_t>(gridDim.x) * kThreads;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < count; i += stride) {
         bf16_t v = 0;
         if (i < a_count) {
@@ -24,7 +29,7 @@ pack_adapter_kernel(const bf16_t* __restrict__ a, const bf16_t* __restrict__ b, 
             const int block = static_cast<int>(f / (k >> 5)), step = static_cast<int>(f % (k >> 5));
             const int r = 16 * block + (lane & 15);
             if (r < rank) v = a[static_cast<int64_t>(r) * k + 32 * step + 8 * (lane >> 4) + e];
-        } else {
+        } else if (i < b_end) {
             const int64_t at = i - a_count;
             const int e = static_cast<int>(at & 7), lane = static_cast<int>(at >> 3) & 63;
             const int64_t f = at >> 9;
@@ -32,156 +37,273 @@ pack_adapter_kernel(const bf16_t* __restrict__ a, const bf16_t* __restrict__ b, 
             const int64_t col = f / blocks * 32 + (lane & 31);
             const int r = 16 * block + 8 * (lane >> 5) + e;
             if (col < n && r < rank) v = b[col * rank + r];
+            v = (v & 0x7f80u) == 0x7f80u ? 0 : v;
         }
         packed[i] = v;
     }
 }
 
-// t[row, s] = weight[row, s] * x[row] A_a^T, a = which[row, s], as `terms` bf16 values that add up to it: the value rounded, what is left of it rounded, and so on (2^-9, 2^-17, 2^-25
-// relative).  One rounding would be as large as that of a bf16 result, and larger where the projection and the adapter cancel.
-// A workgroup owns 16 * RB rows and goes through the blocks of 16 ranks of their distinct adapters, NB at a time; its eight waves split K and meet in LDS, where the sums are formed in wave order.
-// Workgroups of one row tile (blockIdx.y) take turns at the batches.
-constexpr int kDownWaves = 8, kDownAhead = 4;
-template <int RB, int NB>
-__global__ void __launch_bounds__(kDownWaves * 64)
-adapters_down_kernel(const bf16_t* __restrict__ x, const bf16_t* __restrict__ packed, int64_t stride, const int32_t* __restrict__ which, const float* __restrict__ weight, int count, int sel,
-                     int m, int k, int blocks, int terms, int cols, bf16_t* __restrict__ t) {
-    constexpr int ROWS = 16 * RB, F = RB * NB;
-    static_assert(F <= kDownWaves, "a wave per fragment at the end");
-    __shared__ int32_t ids[ROWS * kMostSel];
-    __shared__ __attribute__((aligned(16))) f32x4 sums[kDownWaves - 1][F][64];     // (a wave's own fragment stays in its registers)
-    const int lane = threadIdx.x & 63, l16 = lane & 15, kc = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int m0 = blockIdx.x * ROWS, rows = m - m0 < ROWS ? m - m0 : ROWS, entries = rows * sel;
-    for (int i = threadIdx.x; i < entries; i += kDownWaves * 64) {
-        const int id = which[static_cast<int64_t>(m0) * sel + i];
-        ids[i] = id >= 0 && id < count ? id : kNoAdapter;
-    }
-    __syncthreads();
-    const int steps = k >> 5, per = (steps + kDownWaves - 1) / kDownWaves;
-    const int s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
-    const bf16_t* xp[RB];
-#pragma unroll
-    for (int i = 0; i < RB; ++i) {
-        int row = 16 * i + l16;
-        row = row < rows ? row : rows - 1;                        // rows past the end repeat the last one
-        xp[i] = x + static_cast<int64_t>(m0 + row) * k + 8 * kc;
-    }
-    int a = -1, block = blocks;
-    for (unsigned batch = 0;; ++batch) {
-        int unit_a[NB], unit_block[NB], units = 0;
-#pragma unroll
-        for (int q = 0; q < NB; ++q) {
-            if (block == blocks && a != kNoAdapter) {             // the next adapter: the smallest above the last one
-                int next = kNoAdapter;
-                for (int i = lane; i < entries; i += 64) {
-                    const int id = ids[i];
-                    next = id > a && id < next ? id : next;
-                }
-                next = lanes16_min(next);
-                const int n0 = __builtin_amdgcn_readlane(next, 0), n1 = __builtin_amdgcn_readlane(next, 16), n2 = __builtin_amdgcn_readlane(next, 32), n3 = __builtin_amdgcn_readlane(next, 48);
-                const int lo = n0 < n1 ? n0 : n1, hi = n2 < n3 ? n2 : n3;
-                a = lo < hi ? lo : hi;
-                block = 0;
-            }
-            unit_a[q] = a;
-            unit_block[q] = block;
-            if (a != kNoAdapter) { ++units; ++block; }
+// the columns' bits, a lane per column (behind pack_adapter_kernel, which has made them zeros)
+__global__ void __launch_bounds__(kThreads)
+pack_adapter_bad_kernel(const bf16_t* __restrict__ b, int n, int rank, uint32_t* __restrict__ bad) {
+    const int64_t n_pad = (static_cast<int64_t>(n) + 63) / 64 * 64, stride = static_cast<int64_t>(gridDim.x) * kThreads;
+    const int words = (n + 31) / 32;
+    for (int64_t col = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; col < n_pad; col += stride) {       // (whole waves)
+        bool found = false;
+        if (col < n)
+            for (int r = 0; r < rank; ++r) found = found || (b[col * rank + r] & 0x7f80u) == 0x7f80u;
+        const uint64_t bits = __ballot(found);
+        const int word = static_cast<int>(col >> 5);
+        if ((threadIdx.x & 31) == 0 && word < words) {
+            const uint32_t here = static_cast<uint32_t>(bits >> (threadIdx.x & 32));
+            if (here) { bad[word] = here; bad[words] = 1u; }      // (whoever writes the last word writes the same)
         }
-        if (units == 0) return;
-        if (batch % gridDim.y != blockIdx.y) continue;
-        const bf16_t* wp[NB];
-#pragma unroll
-        for (int q = 0; q < NB; ++q) wp[q] = packed + static_cast<int64_t>(q < units ? unit_a[q] : unit_a[0]) * stride + static_cast<int64_t>(q < units ? unit_block[q] : unit_block[0]) * steps * 512 + lane * 8;
-        f32x4 acc[RB][NB];
-#pragma unroll
-        for (int i = 0; i < RB; ++i)
-#pragma unroll
-            for (int q = 0; q < NB; ++q) acc[i][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int base = s0; base < s1; base += kDownAhead) {
-            bf16x8 xf[kDownAhead][RB], wf[kDownAhead][NB];
-#pragma unroll
-            for (int c = 0; c < kDownAhead; ++c)
-                if (base + c < s1) {
-#pragma unroll
-                    for (int i = 0; i < RB; ++i) xf[c][i] = *reinterpret_cast<const bf16x8*>(xp[i] + (base + c) * 32);
-#pragma unroll
-                    for (int q = 0; q < NB; ++q)
-                        if (q < units) wf[c][q] = *reinterpret_cast<const bf16x8*>(wp[q] + static_cast<int64_t>(base + c) * 512);
-                }
-#pragma unroll
-            for (int c = 0; c < kDownAhead; ++c)
-                if (base + c < s1) {
-#pragma unroll
-                    for (int q = 0; q < NB; ++q)
-                        if (q < units)
-#pragma unroll
-                            for (int i = 0; i < RB; ++i) acc[i][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[c][q], xf[c][i], acc[i][q], 0, 0, 0);
-                }
-        }
-        f32x4 own = f32x4{0.f, 0.f, 0.f, 0.f};
-        int own_a = kNoAdapter, own_block = 0;
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-            if (f == wave) {
-                own = acc[f / NB][f % NB];
-                if (f % NB < units) { own_a = unit_a[f % NB]; own_block = unit_block[f % NB]; }
-            } else {
-                sums[wave < f ? wave : wave - 1][f][lane] = acc[f / NB][f % NB];
-            }
-        }
-        __syncthreads();
-        if (own_a != kNoAdapter) {
-            f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < kDownWaves; ++w) {
-                if (w == wave) sum += own;
-                else sum += sums[w < wave ? w : w - 1][wave][lane];
-            }
-            const int row = 16 * (wave / NB) + l16;
-            if (row < rows)
-                for (int s = 0; s < sel; ++s) {
-                    if (ids[row * sel + s] != own_a) continue;
-                    const int64_t entry = static_cast<int64_t>(m0 + row) * sel + s;
-                    bf16_t* const to = t + entry * cols + 16 * own_block + 4 * kc;
-                    const float w = weight ? weight[entry] : 1.f;
-                    float left[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) left[e] = w * sum[e];
-                    for (int p = 0; p < terms; ++p) {
-                        bf16_t v[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            v[e] = f32_to_bf16(left[e]);
-                            const float r = bf16_to_f32(v[e]);
-                            left[e] = __builtin_fabsf(r) < INFINITY ? left[e] - r : 0.f;       // (what is not finite is one term)
-                        }
-                        *reinterpret_cast<uint2*>(to + p * blocks * 16) = make_uint2(v[0] | static_cast<unsigned>(v[1]) << 16, v[2] | static_cast<unsigned>(v[3]) << 16);
-                    }
-                    if (own_block == blocks - 1 && cols > terms * blocks * 16) *reinterpret_cast<uint2*>(t + entry * cols + terms * blocks * 16 + 4 * kc) = make_uint2(0u, 0u);
-                }
-        }
-        __syncthreads();
     }
 }
 
+// w * x[row] A_a^T, w the sum of the row's weights of adapter a, as `terms` bf16 values that add up to it: the value rounded, what is left of it rounded, and so on (2^-8, 2^-16, 2^-24
+// relative at most).  One rounding would be as large as that of a bf16 result, and larger where the projection and the adapter cancel.
+
+// Four values at ranks 16 * block + 4 * kc on, where at(column) is: the terms' blocks one after the other, filled up to `cols` with zeros.
+template <typename At> __device__ __forceinline__ void put_terms(const At& at, int kc, int block, int blocks, int terms, int cols, float w, const f32x4& sum, bool named = true) {
+    float left[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) left[e] = named ? w * sum[e] : 0.f;
+    for (int p = 0; p < terms; ++p) {
+        bf16_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = f32_to_bf16(left[e]);
+            const float r = bf16_to_f32(v[e]);
+            left[e] = __builtin_fabsf(r) < INFINITY ? left[e] - r : 0.f;           // (what is not finite is one term)
+        }
+        *reinterpret_cast<uint2*>(at((p * blocks + block) * 16 + 4 * kc)) = make_uint2(v[0] | static_cast<unsigned>(v[1]) << 16, v[2] | static_cast<unsigned>(v[3]) << 16);
+    }
+    if (block == blocks - 1 && cols > terms * blocks * 16) *reinterpret_cast<uint2*>(at(terms * blocks * 16 + 4 * kc)) = make_uint2(0u, 0u);
+}
+
+constexpr int kDownWaves = 8;
 struct DownCall { const bf16_t* x; const bf16_t* packed; int64_t stride; const int32_t* which; const float* weight; int count, sel, m, k, blocks, terms, cols; bf16_t* t; };
-template <int RB, int NB>
-int launch_down(regione_ctx* ctx, const DownCall& d) {
-    const int tiles = (d.m + 16 * RB - 1) / (16 * RB);
-    const int64_t most = static_cast<int64_t>(16 * RB) * d.sel < d.count ? static_cast<int64_t>(16 * RB) * d.sel : d.count;      // adapters of a tile
-    const int64_t batches = (most * d.blocks + NB - 1) / NB;
-    int64_t y = (512 + tiles - 1) / tiles;
-    y = y < batches ? y : batches;
-    hipLaunchKernelGGL((adapters_down_kernel<RB, NB>), dim3(static_cast<unsigned>(tiles), static_cast<unsigned>(y)), dim3(kDownWaves * 64), 0, ctx->stream,
-                       d.x, d.packed, d.stride, d.which, d.weight, d.count, d.sel, d.m, d.k, d.blocks, d.terms, d.cols, d.t);
+
+// For the kernel of 16 rows, t [rows, sel, cols], each adapter at the first of the row's places that name it: a workgroup per block of 16 ranks of every place of 16 rows; those whose adapter an earlier place names end at once.  Its eight waves split K and meet in LDS, where the sums are
+// formed in wave order.
+__global__ void __launch_bounds__(kDownWaves * 64)
+adapters_down_rows_kernel(DownCall d) {
+    constexpr int AHEAD = 8;
+    __shared__ __attribute__((aligned(16))) f32x4 sums[kDownWaves][64];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, kc = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m0 = blockIdx.x * 16, rows = d.m - m0 < 16 ? d.m - m0 : 16, entry = blockIdx.y / d.blocks, block = blockIdx.y - entry * d.blocks;
+    if (entry >= rows * d.sel) return;
+    const int32_t* const which = d.which + static_cast<int64_t>(m0) * d.sel;
+    const int a = __builtin_amdgcn_readfirstlane(which[entry]);
+    if (a < 0 || a >= d.count) return;
+    const int steps = d.k >> 5, per = (steps + kDownWaves - 1) / kDownWaves;
+    const int s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
+    const bf16_t* const xp = d.x + static_cast<int64_t>(m0 + (l16 < rows ? l16 : rows - 1)) * d.k + 8 * kc;        // rows past the end repeat the last one
+    const bf16_t* const wp = d.packed + static_cast<int64_t>(a) * d.stride + static_cast<int64_t>(block) * steps * 512 + lane * 8;
+    bf16x8 xf[AHEAD], wf[AHEAD];
+    auto request = [&](int base) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c)
+            if (base + c < s1) {
+                xf[c] = *reinterpret_cast<const bf16x8*>(xp + (base + c) * 32);
+                wf[c] = *reinterpret_cast<const bf16x8*>(wp + static_cast<int64_t>(base + c) * 512);
+            }
+    };
+    request(s0);
+    for (int i = 0; i < entry; i += 64)
+        if (__ballot(i + lane < entry && which[i + lane < entry ? i + lane : 0] == a)) return;      // (the same for all waves)
+    int place = -1;                                               // the row's first place of the adapter, and its weights
+    float w = 0.f;
+    if (l16 < rows)
+        for (int s = d.sel - 1; s >= 0; --s)
+            if (which[l16 * d.sel + s] == a) {
+                place = s;
+                w += d.weight ? d.weight[static_cast<int64_t>(m0 + l16) * d.sel + s] : 1.f;
+            }
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int base = s0; base < s1; base += AHEAD) {
+        if (base > s0) request(base);
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c)
+            if (base + c < s1) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[c], xf[c], acc, 0, 0, 0);
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave || place < 0) return;
+#pragma unroll
+    for (int v = 1; v < kDownWaves; ++v) acc += sums[v][lane];
+    bf16_t* const row = d.t + (static_cast<int64_t>(m0 + l16) * d.sel + place) * d.cols;
+    put_terms([&](int c) { return row + c; }, kc, block, d.blocks, d.terms, d.cols, w, acc);
+}
+
+// For tiles (their layout and plan: gemm_adapters.h): a workgroup owns 16 rows and goes through the blocks of 16 ranks of their adapters, NB at a time; those of the tile that none of the rows
+// names are zeros there.  Workgroups of the same rows (blockIdx.y) take turns.  WAVES waves split K and meet in LDS, where the sums are formed in wave order.
+struct DownTiles { int rows, plan_pitch; int64_t tile_elems; int32_t* plan; int64_t bad; };      // rows of a tile; elements of an adapter ahead of its bits
+template <int NB, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64)
+adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
+    constexpr int AHEAD = 4, T = WAVES * 64;
+    __shared__ uint32_t named[2][kMostAdapters / 32];             // by the tile, by the 16 rows
+    __shared__ int32_t ids[16 * kMostSel];
+    __shared__ float weights[16 * kMostSel];
+    __shared__ __attribute__((aligned(16))) f32x4 sums[WAVES][NB][64];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, kc = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m0 = blockIdx.x * 16, rows = d.m - m0 < 16 ? d.m - m0 : 16;
+    const int tile = m0 / tiles.rows, t0 = tile * tiles.rows, tile_rows = d.m - t0 < tiles.rows ? d.m - t0 : tiles.rows;
+    const int steps = d.k >> 5, per = (steps + WAVES - 1) / WAVES, s0 = wave * per;
+    const int own = s0 + per < steps ? per : (steps > s0 ? steps - s0 : 0);
+    const bf16_t* const xp = d.x + static_cast<int64_t>(m0 + (l16 < rows ? l16 : rows - 1)) * d.k + 8 * kc;        // rows past the end repeat the last one
+    bf16x8 xf[AHEAD], wf[AHEAD][NB];
+    auto step_of = [&](int c) __attribute__((always_inline)) { const int s = s0 + c; return s < steps ? s : steps - 1; };      // (what is past the wave's steps is not multiplied)
+#pragma unroll
+    for (int c = 0; c < AHEAD; ++c) xf[c] = *reinterpret_cast<const bf16x8*>(xp + step_of(c) * 32);
+
+    const int words = (d.count + 31) / 32;
+    for (int i = threadIdx.x; i < words; i += T) named[0][i] = named[1][i] = 0u;
+    __syncthreads();
+    for (int i = threadIdx.x; i < tile_rows * d.sel; i += T) {
+        const int id = d.which[static_cast<int64_t>(t0) * d.sel + i], at = i - (m0 - t0) * d.sel;
+        const bool counts = id >= 0 && id < d.count, here = at >= 0 && at < rows * d.sel;
+        if (counts) {
+            atomicOr(&named[0][id >> 5], 1u << (id & 31));
+            if (here) atomicOr(&named[1][id >> 5], 1u << (id & 31));
+        }
+        if (here) {
+            ids[at] = counts ? id : kNoAdapter;
+            weights[at] = d.weight ? d.weight[static_cast<int64_t>(m0) * d.sel + at] : 1.f;
+        }
+    }
+    __syncthreads();
+
+    unsigned char* const t = reinterpret_cast<unsigned char*>(d.t + tile * tiles.tile_elems);
+    auto place = [&](int row, int half, int c) __attribute__((always_inline)) {       // term c of a half of a step, in the order of LDS
+        return t + (static_cast<int64_t>(half >> 1) * tiles.rows + row) * 128 + ((((half & 1) * 4 + (c >> 3)) ^ ((row >> 1) & 7)) << 4) + (c & 7) * 2;
+    };
+    const int halves = d.cols >> 5, row0 = m0 - t0;
+    const bool lead = m0 == t0 && blockIdx.y == 0;
+    int32_t* const plan = tiles.plan + static_cast<int64_t>(tile) * tiles.plan_pitch;
+    auto zeros = [&](int half, int count) __attribute__((always_inline)) {
+        for (int i = threadIdx.x; i < count * 64; i += T) *reinterpret_cast<uint4*>(place(row0 + (i >> 2 & 15), half + (i >> 6), (i & 3) * 8)) = make_uint4(0u, 0u, 0u, 0u);
+    };
+
+    int a = -1, pos = -1, block = d.blocks;
+    bool in_rows = false;
+    uint32_t bad = 0;
+    auto next_adapter = [&]() __attribute__((always_inline)) {    // the tile's next one, in order
+        int w = (a + 1) >> 5;
+        uint32_t mask = ~0u << ((a + 1) & 31);
+        a = kNoAdapter;
+        while (w < words) {
+            const int at = w + lane;
+            uint32_t v = at < words ? named[0][at] : 0u;
+            if (lane == 0) v &= mask;
+            mask = ~0u;
+            const uint64_t some = __ballot(v != 0u);
+            if (some) {
+                const int first = __builtin_ctzll(some);
+                a = (w + first) * 32 + __builtin_ctz(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(v), first)));
+                break;
+            }
+            w += 64;
+        }
+        if (a == kNoAdapter) return;
+        ++pos;
+        in_rows = named[1][a >> 5] >> (a & 31) & 1u;
+        if (lead) {
+            for (int i = threadIdx.x; i < halves; i += T) {
+                const int first = 2 * i % d.blocks, second = (2 * i + 1) % d.blocks;
+                plan[2 + 2 * (pos * halves + i)] = a;
+                plan[3 + 2 * (pos * halves + i)] = first | second << 16;
+            }
+            if (threadIdx.x == 0) bad |= *reinterpret_cast<const uint32_t*>(d.packed + static_cast<int64_t>(a) * d.stride + tiles.bad);
+        }
+        if (!in_rows && pos % gridDim.y == blockIdx.y) zeros(pos * halves, halves);
+    };
+    bool first_batch = true;
+    for (unsigned batch = 0; a != kNoAdapter; ++batch) {
+        int unit_a[NB], unit_block[NB], unit_pos[NB], units = 0;
+#pragma unroll
+        for (int q = 0; q < NB; ++q) {
+            while (a != kNoAdapter && (block == d.blocks || !in_rows)) { next_adapter(); block = 0; }
+            unit_a[q] = a; unit_block[q] = block; unit_pos[q] = pos;
+            if (a != kNoAdapter) { ++units; ++block; }
+        }
+        if (units == 0 || batch % gridDim.y != blockIdx.y) continue;
+        const bf16_t* wp[NB];
+#pragma unroll
+        for (int q = 0; q < NB; ++q) wp[q] = d.packed + static_cast<int64_t>(q < units ? unit_a[q] : unit_a[0]) * d.stride + static_cast<int64_t>(q < units ? unit_block[q] : unit_block[0]) * steps * 512 + lane * 8;
+        f32x4 acc[NB];
+#pragma unroll
+        for (int q = 0; q < NB; ++q) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < AHEAD; ++c) {
+            const int s = step_of(c);
+            if (!first_batch) xf[c] = *reinterpret_cast<const bf16x8*>(xp + s * 32);
+#pragma unroll
+            for (int q = 0; q < NB; ++q) wf[c][q] = *reinterpret_cast<const bf16x8*>(wp[q] + static_cast<int64_t>(s) * 512);
+        }
+        first_batch = false;
+        for (int base = 0; base < own; base += AHEAD)
+#pragma unroll
+            for (int c = 0; c < AHEAD; ++c) {
+                if (base + c < own)
+#pragma unroll
+                    for (int q = 0; q < NB; ++q) acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[c][q], xf[c], acc[q], 0, 0, 0);
+                const int s = step_of(base + c + AHEAD);
+                xf[c] = *reinterpret_cast<const bf16x8*>(xp + s * 32);
+#pragma unroll
+                for (int q = 0; q < NB; ++q) wf[c][q] = *reinterpret_cast<const bf16x8*>(wp[q] + static_cast<int64_t>(s) * 512);
+            }
+#pragma unroll
+        for (int q = 0; q < NB; ++q) sums[wave][q][lane] = acc[q];
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < NB; ++q)
+            if (q % WAVES == wave && q < units) {
+                f32x4 sum = sums[0][q][lane];
+#pragma unroll
+                for (int v = 1; v < WAVES; ++v) sum += sums[v][q][lane];
+                bool its = false;
+                float w = 0.f;
+                if (l16 < rows)
+                    for (int s = d.sel - 1; s >= 0; --s)
+                        if (ids[l16 * d.sel + s] == unit_a[q]) { its = true; w += weights[l16 * d.sel + s]; }
+                const int half0 = unit_pos[q] * halves;
+                put_terms([&](int c) { return place(row0 + l16, half0 + (c >> 5), c & 31); }, kc, unit_block[q], d.blocks, d.terms, d.cols, w, sum, its);
+            }
+        __syncthreads();
+    }
+    const int all = (pos + 1) * halves;
+    if ((all & 1) && blockIdx.y == 0) zeros(all, 1);              // the last step's second half
+    if (lead && threadIdx.x == 0) {
+        plan[0] = all;
+        plan[1] = static_cast<int32_t>(bad);
+        if (all & 1) { plan[2 + 2 * all] = plan[2 + 2 * (all - 1)]; plan[3 + 2 * all] = 0; }
+    }
+}
+
+int down_rows(regione_ctx* ctx, const DownCall& d) {
+    hipLaunchKernelGGL(adapters_down_rows_kernel, dim3(static_cast<unsigned>((d.m + 15) / 16), static_cast<unsigned>((d.m < 16 ? d.m : 16) * d.sel * d.blocks)), dim3(kDownWaves * 64), 0, ctx->stream, d);
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }
-int down(regione_ctx* ctx, const DownCall& d) {
-    if (d.m <= 512) return launch_down<1, 1>(ctx, d);
-    if (d.m <= 4096) return launch_down<1, 4>(ctx, d);
-    return launch_down<2, 4>(ctx, d);
+
+constexpr int kDownFew = 128;                                    // pieces of 16 rows up to which every block of ranks has workgroups of its own
+int down_tiles(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
+    const int pieces = (d.m + 15) / 16;
+    const int64_t most = static_cast<int64_t>(16) * d.sel < d.count ? static_cast<int64_t>(16) * d.sel : d.count, units = most * d.blocks;      // of 16 rows
+    const int64_t room = pieces < 1024 ? 1024 / pieces : 1;
+    if (pieces <= kDownFew) {
+        hipLaunchKernelGGL((adapters_down_tiles_kernel<1, 8>), dim3(pieces, static_cast<unsigned>(units < room ? units : room)), dim3(512), 0, ctx->stream, d, tiles);
+    } else {
+        const int64_t batches = (units + 3) / 4;
+        hipLaunchKernelGGL((adapters_down_tiles_kernel<4, 4>), dim3(pieces, static_cast<unsigned>(batches < room ? batches : room)), dim3(256), 0, ctx->stream, d, tiles);
+    }
+    RG_LAUNCH_CHECK();
+    return REGIONE_OK;
 }
 
 }  // namespace
@@ -211,6 +333,10 @@ extern "C" int regione_pack_adapter(regione_ctx* ctx, const void* a, const void*
     hipLaunchKernelGGL(pack_adapter_kernel, dim3(static_cast<unsigned>(grid)), dim3(kThreads), 0, ctx->stream, static_cast<const bf16_t*>(a), static_cast<const bf16_t*>(b), n, k, rank, blocks,
                        static_cast<bf16_t*>(packed));
     RG_LAUNCH_CHECK();
+    grid = (static_cast<int64_t>(n) + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL(pack_adapter_bad_kernel, dim3(static_cast<unsigned>(grid < 256 * 32 ? grid : 256 * 32)), dim3(kThreads), 0, ctx->stream, static_cast<const bf16_t*>(b), n, rank,
+                       reinterpret_cast<uint32_t*>(static_cast<bf16_t*>(packed) + a_elems(k, blocks) + b_elems(n, blocks)));
+    RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }
 
@@ -231,27 +357,52 @@ extern "C" int regione_linear_adapters(regione_ctx* ctx, const void* x, const vo
 
     const bool y_f32 = out_dtype == REGIONE_FP32;
     const int blocks = (rank + 15) / 16, terms = y_f32 ? 3 : 2, cols = (terms * blocks * 16 + 31) & ~31;
-    const size_t row_bytes = static_cast<size_t>(n_sel) * cols * 2;
-    int64_t most = static_cast<int64_t>(kTermBytes / row_bytes) & ~int64_t{255};             // (at least 512: 32 adapters of rank 256 in three terms)
-    const int64_t chunk = m < most ? m : most;
-    const size_t bytes = (static_cast<size_t>(chunk) * row_bytes + 255) & ~size_t{255}, all = ctx->gemm_part_bytes;
-    if (bytes > all) RG_FAIL(REGIONE_ERR_WORKSPACE, "linear_adapters: %zu bytes of inner products exceed the workspace of %zu", bytes, all);
-    ProfScope prof(ctx, REGIONE_PROF_GEMM);
+    const size_t all = ctx->gemm_part_bytes, room = all / 2 < kTermBytes ? (all / 2) & ~size_t{255} : kTermBytes;      // (a context without a workspace has none)
     // the inner products lie at the workspace's end, the sums of K splits in the rest of it
-    bf16_t* const t = reinterpret_cast<bf16_t*>(reinterpret_cast<char*>(ctx->gemm_part) + all - bytes);
-    ctx->gemm_part_bytes = all - bytes;
+    char* const end = reinterpret_cast<char*>(ctx->gemm_part) + all - room;
+    ctx->gemm_part_bytes = all - room;
+    AdapterTiles tiles = rg_adapter_tiles(ctx, m, n, k);
+    // the most that a tile can name: every row another adapter
+    const int64_t named = static_cast<int64_t>(tiles.rows) * n_sel < n_adapters ? static_cast<int64_t>(tiles.rows) * n_sel : n_adapters, tile_steps = (named * (cols / 32) + 1) / 2;
+    const int64_t tile_bytes = tile_steps * tiles.rows * 128, plan_bytes = (2 + 4 * tile_steps) * 4, fits = static_cast<int64_t>(room) / (tile_bytes + plan_bytes), m_tiles = (m + tiles.rows - 1) / tiles.rows;
+    int64_t chunk = m;
+    if (tiles.tile && fits < m_tiles) {
+        if (fits * tiles.rows >= kLeastChunk) {
+            chunk = fits * tiles.rows;
+            tiles.splits = 1;
+        } else {
+            tiles = {0, 1, 16};                                   // the kernel of 16 rows reads what its rows name and no more
+        }
+    }
+    const size_t row_bytes = static_cast<size_t>(n_sel) * cols * 2;
+    if (!tiles.tile) {
+        const int64_t most = static_cast<int64_t>(room / row_bytes) & ~int64_t{15};
+        chunk = m < most ? m : most;
+    }
     int rc = REGIONE_OK;
+    if (chunk <= 0) {
+        rc = REGIONE_ERR_WORKSPACE;
+        regione_set_error("linear_adapters: the inner products of a row, %zu bytes, need a workspace", row_bytes);
+    }
+    ProfScope prof(ctx, REGIONE_PROF_GEMM);
     for (int64_t r0 = 0; r0 < m && rc == REGIONE_OK; r0 += chunk) {
         const int rows = static_cast<int>(m - r0 < chunk ? m - r0 : chunk);
         DownCall d = {static_cast<const bf16_t*>(x) + r0 * k, static_cast<const bf16_t*>(adapters_packed), adapter_elems(n, k, blocks), adapter + r0 * n_sel, weight_opt ? weight_opt + r0 * n_sel : nullptr,
-                      n_adapters, n_sel, rows, k, blocks, terms, cols, t};
-        rc = down(ctx, d);
-        if (rc != REGIONE_OK) break;
+                      n_adapters, n_sel, rows, k, blocks, terms, cols, reinterpret_cast<bf16_t*>(end)};
         GemmEpilogue ep = {};
         ep.kind = EPI_PLAIN; ep.bias = b_opt; ep.act = act; ep.act_from = 0;
         ep.y = static_cast<char*>(y) + r0 * n * (y_f32 ? 4 : 2); ep.ldy = n; ep.y_f32 = y_f32;
-        ep.adapters = {t, d.which, d.packed + a_elems(k, blocks), d.stride, n_sel, n_adapters, cols, blocks};
-        rc = rg_gemm_adapters(ctx, d.x, k, w_packed, rows, n, k, ep);
+        const bf16_t* const b = d.packed + a_elems(k, blocks);
+        ep.adapters = {d.t, d.which, b, reinterpret_cast<const uint32_t*>(b + b_elems(n, blocks)), d.stride, n_sel, n_adapters, cols, blocks, nullptr, 0, 0};
+        if (tiles.tile) {
+            const int64_t parts = (rows + tiles.rows - 1) / tiles.rows;
+            DownTiles at = {tiles.rows, static_cast<int>(2 + 4 * tile_steps), tile_bytes / 2, reinterpret_cast<int32_t*>(end + parts * tile_bytes), a_elems(k, blocks) + b_elems(n, blocks) + 2 * ((static_cast<int64_t>(n) + 31) / 32)};
+            ep.adapters.plan = at.plan; ep.adapters.plan_pitch = at.plan_pitch; ep.adapters.tile_elems = at.tile_elems;
+            rc = down_tiles(ctx, d, at);
+        } else {
+            rc = down_rows(ctx, d);
+        }
+        if (rc == REGIONE_OK) rc = rg_gemm_adapters(ctx, tiles, d.x, k, w_packed, rows, n, k, ep);
     }
     ctx->gemm_part_bytes = all;
     return rc;

@@ -104,11 +104,13 @@ __device__ __forceinline__ bf16_t f32_to_bf16(float f) {
 }
 
 // ---- internal launchers (each enqueues on ctx->stream and returns an error code)
-enum { EPI_PLAIN = 0, EPI_QKV = 1, EPI_RESID = 2, EPI_VELOCITY = 3, EPI_ADAPTERS = 4 };      // EPI_ADAPTERS: EPI_PLAIN behind adapters_add (gemm_adapters.h)
+enum { EPI_PLAIN = 0, EPI_QKV = 1, EPI_RESID = 2, EPI_VELOCITY = 3, EPI_ADAPTERS = 4 };      // EPI_ADAPTERS: EPI_PLAIN behind the adapters' share (gemm_adapters.h)
 
-// Low-rank adapters of a product's rows: t [rows, sel, cols] the inner products with A in bf16 terms, which [rows, sel] their adapters (none: outside [0, count)), b the packed B of
-// adapter 0, those of the others `stride` elements further each; blocks: of 16 ranks; cols: the terms' blocks, filled up to 32 with zeros.
-struct AdapterRows { const bf16_t* t; const int32_t* which; const bf16_t* b; int64_t stride; int sel, count, cols, blocks; };
+// Low-rank adapters of a product's rows (gemm_adapters.h): which [rows, sel] their adapters (none: outside [0, count)), b the packed B of adapter 0 and bad the bits of its columns that hold
+// values that are not finite, those of the others `stride` elements further each; blocks: of 16 ranks; cols: the terms' blocks, filled up to 32 with zeros.  t: the inner products with A in
+// bf16 terms, [rows, sel, cols] for the kernel of 16 rows, tile by tile with a plan for the others.
+struct AdapterRows { const bf16_t* t; const int32_t* which; const bf16_t* b; const uint32_t* bad; int64_t stride; int sel, count, cols, blocks; const int32_t* plan; int plan_pitch; int64_t tile_elems; };
+struct AdapterTiles { int tile, splits, rows; };                 // the product's tile and its rows; tile 0: the kernel of 16 rows
 
 struct GemmEpilogue {
     int kind;            // EPI_*
@@ -162,7 +164,8 @@ struct VecBatch { const float* x[kModSets]; const bf16_t* w[kModSets]; const flo
 static inline bool rg_vec_columns_ok(int k) { return k % 8 == 0 && k <= 16384; }      // whole 16-byte pieces, and the vector as float32 within 64 KiB of LDS
 int rg_vec_linear_batch(regione_ctx* ctx, VecBatch& batch, int k, const int32_t* go);
 // y = act(x W^T + b + adapters), ep as for a plain product
-int rg_gemm_adapters(regione_ctx* ctx, const bf16_t* a, int lda, const void* w_packed, int m, int n, int k, const GemmEpilogue& ep);
+AdapterTiles rg_adapter_tiles(regione_ctx* ctx, int m, int n, int k);
+int rg_gemm_adapters(regione_ctx* ctx, const AdapterTiles& tiles, const bf16_t* a, int lda, const void* wp, int m, int n, int k, const GemmEpilogue& ep);
 // One product: norm: of layernorm_mod(a), rows a of k values (a_f32: float32).
 struct GemmCall { const void* a; int lda, norm, a_f32; const float* shift; const float* scale; const void* w; int m, n, k; GemmEpilogue ep; };
 // Two products of the same shape but for their rows (the text and the image rows of a block, each with weights of their own) in one launch, with the results of two calls bit for

@@ -272,16 +272,20 @@ int rg_gemm(regione_ctx* ctx, const void* a_any, int lda, const void* wp_any, in
     return gemm_tile(ctx, plan_gemm(ctx, m, n, k, ep.keep_sums ? PLAN_KEPT : PLAN_BF16), a, lda, wp, m, n, k, ep);
 }
 
-int rg_gemm_adapters(regione_ctx* ctx, const bf16_t* a, int lda, const void* wp_any, int m, int n, int k, const GemmEpilogue& ep_in) {
+AdapterTiles rg_adapter_tiles(regione_ctx* ctx, int m, int n, int k) {
+    if (small_columns(ctx, m, n, k)) return {0, 1, 16};
+    const GemmPlan p = plan_gemm(ctx, m, n, k, PLAN_BF16);
+    return {p.tile, p.splits, p.tile < 100 ? 32 * (p.tile / 10) : 16 * (p.tile / 10 % 10) * (p.tile / 100)};
+}
+
+int rg_gemm_adapters(regione_ctx* ctx, const AdapterTiles& tiles, const bf16_t* a, int lda, const void* wp_any, int m, int n, int k, const GemmEpilogue& ep_in) {
     if (m <= 0 || n <= 0) return REGIONE_OK;
     const bf16_t* wp = static_cast<const bf16_t*>(wp_any);
     GemmEpilogue ep = ep_in;
     ep.vec_ok = (n % 8 == 0) && wide_epilogue_ok(ep, n);
     ep.kind = EPI_ADAPTERS;
-    if (const int columns = small_columns(ctx, m, n, k))
-        return columns == 32 ? launch_small<2, EPI_ADAPTERS, LN_NONE>(ctx, a, lda, wp, m, n, k, nullptr, nullptr, ep) : launch_small<4, EPI_ADAPTERS, LN_NONE>(ctx, a, lda, wp, m, n, k, nullptr, nullptr, ep);
-    const GemmPlan p = plan_gemm(ctx, m, n, k, PLAN_BF16);
-    return rg_gemm_tile_adapters(ctx, p.tile, a, lda, wp, m, n, k, p.splits, ep);
+    if (tiles.tile) return rg_gemm_tile_adapters(ctx, tiles.tile, a, lda, wp, m, n, k, tiles.splits, ep);
+    return small_columns(m, n, k, false) == 32 ? launch_small<2, EPI_ADAPTERS, LN_NONE>(ctx, a, lda, wp, m, n, k, nullptr, nullptr, ep) : launch_small<4, EPI_ADAPTERS, LN_NONE>(ctx, a, lda, wp, m, n, k, nullptr, nullptr, ep);
 }
 
 int rg_layernorm_gemm(regione_ctx* ctx, const void* h, int h_f32, const float* shift, const float* scale, void* u, const void* wp, int m, int n, int k, const GemmEpilogue& ep_in) {

@@ -1,109 +1,146 @@
-// Low-rank adapters beside a projection, at the end of the projection's tiles: y[r] += sum over s of (weight[r, s] x[r] A_a^T) B_a^T, a = which[r, s].
+// Low-rank adapters beside a projection, in the projection's kernels: y[r] += sum over s of (weight[r, s] x[r] A_a^T) B_a^T, a = which[r, s].
 //
-// The inner products with A, times their weights, are there already (adapters.hip): rows t[r, s] of bf16 terms that add up to them, `blocks` blocks of 16 ranks per term, so that a row of
-// t times [B_a | B_a | ..] is the adapter's share of the result.  A wave multiplies the rows of its fragments with one adapter after the other, those of other adapters as zeros, into the
-// accumulators that hold the projection's sums: nothing is written or read in between, and the result is rounded once.
+// The inner products with A, times their weights, are there already (adapters.hip) as bf16 terms that add up to them, `blocks` blocks of 16 ranks per term, so that a row of terms times
+// [B_a | B_a | ..] is the adapter's share of the result.  An adapter that a row names more than once has its weights added up.  The share is summed in the accumulators that hold the
+// projection's sums: nothing is written or read in between, and the result is rounded once.
+//
+// Tiles (gemm_pp.h) take the terms as K-steps behind the product's own: for every adapter that a row of the tile names, in ascending order, its terms in all of the tile's rows, zeros in those
+// that do not name it, in the order that a step has in LDS, the tile's steps one after the other.  The plan of a tile: the number of its halves of steps (32 terms), whether one of its
+// adapters has values in B that are not finite, and for each half the adapter and the two blocks of 16 ranks of B that it meets.  As steps of the same loop they cost what K costs, and their
+// first loads fly under the product's last steps.  Summed at the end of the tile, each wave its rows and their adapters, they waited for memory step by step, 1.7 us each.
+// Rows without the adapter must not see its values (zero times infinity): what is not finite in B is zero in the packed adapter, and the columns that hold such values are spoilt at the end,
+// in the rows that name the adapter.
 #pragma once
 #include "gemm_epilogue.h"
 
 namespace {
 
-// the smallest of a value's 16 lanes, in all of them
-__device__ __forceinline__ int lanes16_min(int v) {
-    auto less = [](int a, int b) { return a < b ? a : b; };
-    v = less(v, __builtin_amdgcn_update_dpp(v, v, 0x121, 0xf, 0xf, false));       // row_ror 1, 2, 4, 8
-    v = less(v, __builtin_amdgcn_update_dpp(v, v, 0x122, 0xf, 0xf, false));
-    v = less(v, __builtin_amdgcn_update_dpp(v, v, 0x124, 0xf, 0xf, false));
-    return less(v, __builtin_amdgcn_update_dpp(v, v, 0x128, 0xf, 0xf, false));
+typedef const __attribute__((address_space(4))) int32_t* AdapterPlan;          // read by the scalar unit: no vector load among the counted copies
+__device__ __forceinline__ AdapterPlan adapter_plan(const AdapterRows& ad, int tile) { return (AdapterPlan)(ad.plan + static_cast<int64_t>(tile) * ad.plan_pitch); }
+__device__ __forceinline__ int adapter_steps(AdapterPlan plan) { return (plan[0] + 1) >> 1; }
+__device__ __forceinline__ const char* adapter_terms(const AdapterRows& ad, int tile) { return reinterpret_cast<const char*>(ad.t + tile * ad.tile_elems); }
+// a half of a step: its adapter and the two blocks of 16 ranks of B that its terms meet
+struct AdapterHalf { int id, blocks; };
+__device__ __forceinline__ AdapterHalf adapter_half(AdapterPlan plan, int half) { return {plan[2 + 2 * half], plan[3 + 2 * half]}; }
+// 32 columns x 16 ranks of B: block j of the half, column block nb
+__device__ __forceinline__ const char* adapter_block(const AdapterRows& ad, const AdapterHalf& half, int j, int nb) {
+    return reinterpret_cast<const char*>(ad.b + half.id * ad.stride + (static_cast<int64_t>(nb) * ad.blocks + (j ? half.blocks >> 16 : half.blocks & 0xffff)) * 512);
 }
-constexpr int kNoAdapter = 0x7fffffff;
+// the bits of 32 columns of an adapter
+__device__ __forceinline__ uint32_t adapter_bad(const AdapterRows& ad, int id, int nb) { return ad.bad[(static_cast<int64_t>(id) * ad.stride >> 1) + nb]; }
 
-// Rows [I0, I1) of a wave's fragments, in the layout of gemm_epilogue16.  turn, turns: of the steps of 32 terms, counted over all adapters, this wave takes those numbered turn modulo turns
-// (where several waves add up the same fragments).
-// Rows without the adapter must not see its values (zero times infinity): the fragments that hold such rows take the instruction's result for their own rows only.
-template <int I0, int I1, int RF, int CF>
-__device__ __forceinline__ void adapters_add(f32x4 (&acc)[RF][CF], int M, int N, int m0, int n0w, const AdapterRows& ad, int turn = 0, int turns = 1) {
-    constexpr int R = I1 - I0;
-    const int lane = threadIdx.x & 63, l16 = lane & 15, kc = lane >> 4;
-    const int last_block = ((N + 31) >> 5) - 1, steps = ad.cols >> 5;
-    // weight fragment j of a lane: column 8*(l16/4) + 4*(j%2) + l16%4 of block j / 2, as the epilogue expects it
-    int64_t w_at[CF / 2];
+// Rows [I0, I1) of a wave's fragments, in the layout of gemm_epilogue16: columns of adapters that hold values that are not finite, in the rows that name the adapter.
+template <int I0, int I1, int RF, int CF> __device__ __forceinline__ void adapters_spoil(f32x4 (&acc)[RF][CF], int M, int N, int m0, int n0w, const AdapterRows& ad, AdapterPlan plan) {
+    if (plan[1] == 0) return;
+    const int lane = threadIdx.x & 63, last_block = ((N + 31) >> 5) - 1, halves = plan[0];
+    int last = -1;
+#pragma unroll 1
+    for (int h = 0; h < halves; ++h) {
+        const int id = plan[2 + 2 * h];
+        if (id == last) continue;
+        last = id;
+        unsigned bad[CF / 2], any = 0;                            // of the lane's eight columns
+#pragma unroll
+        for (int b = 0; b < CF / 2; ++b) {
+            const int nb = (n0w >> 5) + b;
+            bad[b] = adapter_bad(ad, id, nb < last_block ? nb : last_block) >> (8 * (lane >> 4));
+            any |= bad[b] & 0xffu;
+        }
+        if (!__ballot(any != 0)) continue;
+#pragma unroll
+        for (int i = I0; i < I1; ++i) {
+            const int row = m0 + 16 * i + (lane & 15);
+            bool named = false;
+            if (row < M)
+                for (int s = 0; s < ad.sel; ++s) named = named || ad.which[static_cast<int64_t>(row) * ad.sel + s] == id;
+#pragma unroll
+            for (int j = 0; j < CF; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = named && (bad[j >> 1] >> (4 * (j & 1) + e)) & 1 ? __builtin_nanf("") : acc[i][j][e];
+        }
+    }
+}
+
+// Weight fragment j of a lane: column 8*(l16/4) + 4*(j%2) + l16%4 of the 32 columns' block j / 2, as the epilogue expects it, and the 16 terms of its half of a step, from `block0` on.
+template <int CF> __device__ __forceinline__ void adapter_weights(const AdapterRows& ad, int a, int N, int n0, int block0, bf16x8 (&w)[CF]) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, kc = lane >> 4, last_block = ((N + 31) >> 5) - 1;
+    int block = block0 + (kc >> 1);
+    block = block < ad.blocks ? block : block - ad.blocks;
+    const int at = block * 512 + ((kc & 1) * 32 + 8 * (l16 >> 2) + (l16 & 3)) * 8;
 #pragma unroll
     for (int b = 0; b < CF / 2; ++b) {
-        int nb = (n0w >> 5) + b;
+        int nb = __builtin_amdgcn_readfirstlane(n0 >> 5) + b;
         nb = nb < last_block ? nb : last_block;                   // blocks past N repeat the last one; their sums are not stored
-        w_at[b] = (static_cast<int64_t>(nb) * ad.blocks * 64 + (kc & 1) * 32 + 8 * (l16 >> 2) + (l16 & 3)) * 8;
-    }
-    // rows of terms, all of them within 32 MB; those past M are zero by the resource's size
-    const auto terms = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(ad.t), 0, M * ad.sel * ad.cols * 2, 0x00027000);
-    const unsigned t_rows = 16u * ad.sel * ad.cols * 2u, t_first = static_cast<unsigned>((m0 + 16 * I0 + l16) * ad.sel * ad.cols + 8 * kc) * 2u;
-    // One loop over all steps of all adapters, the smallest number first: nested ones leave the compiler with a copy of the accumulators for each.
-    int step_no = 0, s = 0, a = -1, st = steps - 1, first_block = 0;
-    int id[R];
-    auto load_ids = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int row = m0 + 16 * (I0 + i) + l16;
-            id[i] = row < M ? ad.which[row * ad.sel + s] : -1;
-            if (id[i] >= ad.count) id[i] = -1;
-        }
-    };
-    load_ids();
-    // the next step; false behind the last one
-    auto go = [&]() __attribute__((always_inline)) {
-        if (++st < steps) {
-            first_block += 2;
-            while (first_block >= ad.blocks) first_block -= ad.blocks;
-            return true;
-        }
-        st = first_block = 0;
-        int next = kNoAdapter;
-#pragma unroll 1
-        while (true) {
-#pragma unroll
-            for (int i = 0; i < R; ++i) next = id[i] > a && id[i] < next ? id[i] : next;
-            next = __builtin_amdgcn_readfirstlane(lanes16_min(next));
-            if (next != kNoAdapter || ++s >= ad.sel) break;
-            load_ids();
-            a = -1;
-        }
-        a = next;
-        return next != kNoAdapter;
-    };
-    bool more = go();
-#pragma unroll 1
-    while (more) {
-        if (turns == 1 || step_no++ % turns == turn) {
-            const unsigned t_at = t_first + static_cast<unsigned>(s * ad.cols + 32 * st) * 2u;
-            const bf16_t* const b = ad.b + static_cast<int64_t>(a) * ad.stride;
-            int block = first_block + (kc >> 1);
-            block = block < ad.blocks ? block : block - ad.blocks;
-            bf16x8 wf[CF];
-#pragma unroll
-            for (int j = 0; j < CF; ++j) wf[j] = *reinterpret_cast<const bf16x8*>(b + w_at[j / 2] + block * 512 + (j & 1) * 32);
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                u32x4 tr = __builtin_amdgcn_raw_buffer_load_b128(terms, t_at + i * t_rows, 0, 0);
-                const bool mine = id[i] == a;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) tr[e] = mine ? tr[e] : 0u;
-#pragma unroll
-                for (int j = 0; j < CF; ++j) {
-                    const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], __builtin_bit_cast(bf16x8, tr), acc[I0 + i][j], 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[I0 + i][j][e] = mine ? sum[e] : acc[I0 + i][j][e];
-                }
-#pragma unroll
-                for (int j = 0; j < CF; ++j) {
-                    f32x4 here = acc[I0 + i][j];              // here, and not behind all rows' instructions with all their results in registers
-                    asm volatile("" : "+v"(here));
-                    acc[I0 + i][j] = here;
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        }
-        more = go();
+        const bf16_t* const from = ad.b + static_cast<int64_t>(a) * ad.stride + static_cast<int64_t>(nb) * ad.blocks * 512;
+        w[2 * b] = *reinterpret_cast<const bf16x8*>(from + at);
+        w[2 * b + 1] = *reinterpret_cast<const bf16x8*>(from + at + 32);
     }
 }
+// rows of terms, all of them within 32 MB; what lies outside, such as no place at all, is zero by the resource's size
+__device__ __forceinline__ auto adapter_terms_rsrc(const AdapterRows& ad, int M) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(ad.t), 0, M * ad.sel * ad.cols * 2, 0x00027000); }
+constexpr unsigned kNoTerms = 0xfffffff0u;
+
+// For the 16 rows that several waves share (gemm_small.h): t [rows, sel, cols], each adapter's terms at the first of the row's places that name it.  A unit of work is a step of 32 terms of an
+// adapter that no earlier row or place of the tile names; wave `turn` of `turns` takes every unit that is its turn.  The first units' operands are requested ahead of the product (fetch, then
+// add behind it).
+template <int CF> struct AdapterUnits {
+    static constexpr int AHEAD = 2;
+    bf16x8 wf[AHEAD][CF];
+    u32x4 tf[AHEAD];
+    unsigned bad[AHEAD][CF / 2];                                  // of the lane's columns, where its row names the adapter
+    bool there[AHEAD];
+    int next;
+
+    __device__ __forceinline__ void load(const AdapterRows& ad, int M, int N, int m0, int n0, int q, int unit, int units, int turns) {
+        const int lane = threadIdx.x & 63, l16 = lane & 15, kc = lane >> 4, steps = ad.cols >> 5;
+        there[q] = false;
+        const int rows = M - m0 < 16 ? M - m0 : 16;
+        const int32_t* const which = ad.which + static_cast<int64_t>(m0) * ad.sel;
+        if (unit >= units) return;
+        const int entry = unit / steps, st = unit - entry * steps;
+        const int a = __builtin_amdgcn_readfirstlane(which[entry]);
+        if (a < 0 || a >= ad.count) return;
+        for (int i = 0; i < entry; i += 64)                       // named before?
+            if (__ballot(i + lane < entry && which[i + lane < entry ? i + lane : 0] == a)) return;
+        unsigned at = kNoTerms;
+        if (l16 < rows)
+            for (int s = ad.sel - 1; s >= 0; --s)
+                if (which[l16 * ad.sel + s] == a) at = (static_cast<unsigned>(m0 + l16) * ad.sel + s) * (ad.cols * 2u) + 64u * st + 16u * kc;
+        there[q] = true;
+        tf[q] = __builtin_amdgcn_raw_buffer_load_b128(adapter_terms_rsrc(ad, M), at, 0, 0);
+        adapter_weights<CF>(ad, a, N, n0, 2 * st % ad.blocks, wf[q]);
+        const int last_block = ((N + 31) >> 5) - 1;
+#pragma unroll
+        for (int b = 0; b < CF / 2; ++b) {
+            const int nb = (n0 >> 5) + b;
+            bad[q][b] = adapter_bad(ad, a, nb < last_block ? nb : last_block);
+            bad[q][b] = st == 0 && at != kNoTerms ? bad[q][b] >> (8 * kc) : 0u;
+        }
+    }
+    __device__ __forceinline__ void use(f32x4 (&acc)[CF], int q) {
+        if (!there[q]) return;
+#pragma unroll
+        for (int j = 0; j < CF; ++j) {
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[q][j], __builtin_bit_cast(bf16x8, tf[q]), acc[j], 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[j][e] = (bad[q][j >> 1] >> (4 * (j & 1) + e)) & 1 ? __builtin_nanf("") : acc[j][e];
+        }
+    }
+    __device__ __forceinline__ void fetch(const AdapterRows& ad, int M, int N, int m0, int n0, int turn, int turns) {
+        const int units = (M - m0 < 16 ? M - m0 : 16) * ad.sel * (ad.cols >> 5);
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) load(ad, M, N, m0, n0, q, turn + q * turns, units, turns);
+        next = turn + AHEAD * turns;
+    }
+    __device__ __forceinline__ void add(f32x4 (&acc)[CF], const AdapterRows& ad, int M, int N, int m0, int n0, int turns) {
+        const int units = (M - m0 < 16 ? M - m0 : 16) * ad.sel * (ad.cols >> 5);
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) use(acc, q);
+        for (int unit = next; unit < units; unit += turns) {
+            load(ad, M, N, m0, n0, 0, unit, units, turns);
+            use(acc, 0);
+        }
+    }
+};
 
 }  // namespace

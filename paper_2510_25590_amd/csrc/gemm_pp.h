@@ -72,7 +72,7 @@ constexpr int pp_group(int F) { int g = F < 8 ? F : 8; while (F % g) --g; return
 // is last) and goes on to the epilogue.  Nobody waits.  wave_slot: the wave's place among the tile's WAVES fragment sets.
 template <int I0, int I1, int RF, int CF, int KIND, bool FP8>
 __device__ __forceinline__ void pp_finish(f32x4 (&acc)[RF][CF], unsigned char* lds_raw, int wave_slot, int64_t part_floats, int tile, int split, int splits,
-                                          float* __restrict__ partial, int* __restrict__ arrived, int M, int N, int m0, int n0w, const GemmEpilogue& ep) {
+                                          float* __restrict__ partial, int* __restrict__ arrived, int M, int N, int m0, int n0w, const GemmEpilogue& ep, AdapterPlan plan = nullptr) {
     const int lane = threadIdx.x & 63;
     if (splits > 1) {
         const auto rsrc = pp_part_rsrc(partial + static_cast<int64_t>(tile) * splits * part_floats, splits * part_floats);
@@ -121,7 +121,7 @@ __device__ __forceinline__ void pp_finish(f32x4 (&acc)[RF][CF], unsigned char* l
             }
     }
     if constexpr (KIND == EPI_ADAPTERS) {
-        adapters_add<I0, I1, RF, CF>(acc, M, N, m0, n0w, ep.adapters);
+        adapters_spoil<I0, I1, RF, CF>(acc, M, N, m0, n0w, ep.adapters, plan);
         gemm_epilogue16<EPI_PLAIN, FP8, I0, I1, RF, CF>(acc, M, N, m0, n0w, ep);
     } else {
         gemm_epilogue16<KIND, FP8, I0, I1, RF, CF>(acc, M, N, m0, n0w, ep);
@@ -168,6 +168,13 @@ gemm_pp_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
     const int ks_begin = split * steps_per_split;
     int n_steps = K / 64 - ks_begin;
     n_steps = n_steps < steps_per_split ? n_steps : steps_per_split;
+    // low-rank adapters: their K-steps follow the product's own
+    const int n_own = n_steps;
+    AdapterPlan plan = nullptr;
+    if constexpr (KIND == EPI_ADAPTERS) {
+        plan = adapter_plan(ep.adapters, m_tile);
+        if (split == splits - 1) n_steps += adapter_steps(plan);
+    }
     const int n_phases = n_steps * (2 / HP);
 
     // Copy sources.  A: a lane copies 16 bytes of one row; LDS rows are 128 bytes, 16-byte chunk c of row r at c ^ ((r >> 1) & 7),
@@ -227,12 +234,34 @@ gemm_pp_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
         ++w_next; w_slot = w_slot == (T::W_SLOTS - 1) * T::W_SLOT ? 0 : w_slot + T::W_SLOT;                 \
     }
 #define PP_WAIT() { pp_wait<PENDING>(); __builtin_amdgcn_sched_barrier(0); }
-    PP_COPY_A(0, AC) PP_A_DONE() PP_COPY_W()
+    // the same copies where they may be those of adapters' steps, whose rows come in the order of LDS and whose weights lie where the plan says
+    const char* const t_base = KIND == EPI_ADAPTERS ? adapter_terms(ep.adapters, m_tile) + wave * (AC * 1024) : nullptr;
+#define PP_COPY_A_END(I0, I1)                                                                               \
+    if constexpr (KIND == EPI_ADAPTERS) {                                                                   \
+        const int st_ = a_next < n_steps ? a_next : n_steps - 1;                                            \
+        const bool theirs_ = st_ >= n_own;                                                                  \
+        const char* src_ = theirs_ ? t_base + static_cast<int64_t>(st_ - n_own) * T::A_STEP : a_base + static_cast<int64_t>(st_) * 128; \
+        unsigned off_[AC];                                                                                  \
+        _Pragma("unroll") for (int i = 0; i < AC; ++i) off_[i] = theirs_ ? static_cast<unsigned>(lane) * 16u + i * 1024u : a_voff[i]; \
+        pp_copies_if<I0, I1>(off_, src_, a_dst + a_buf, a_live);                                            \
+    } else PP_COPY_A(I0, I1)
+#define PP_COPY_W_END()                                                                                     \
+    if constexpr (KIND == EPI_ADAPTERS) {                                                                   \
+        static_assert(WC == KB, "a wave copies a phase's k-blocks of one column block");                    \
+        const int ph_ = w_next < n_phases ? w_next : n_phases - 1, half_ = (ph_ - n_own * (2 / HP)) * HP;   \
+        const char* const src_ = w_base + static_cast<int64_t>(ph_) * (KB * 1024);                          \
+        _Pragma("unroll") for (int c = 0; c < WC; ++c) {                                                    \
+            const char* const theirs_ = adapter_block(ep.adapters, adapter_half(plan, (half_ < 0 ? 0 : half_) + (c >> 1)), c & 1, nb); \
+            pp_copy16(w_voff, half_ >= 0 ? theirs_ : src_ + c * 1024, w_dst + w_slot + c * 1024u);          \
+        }                                                                                                   \
+        ++w_next; w_slot = w_slot == (T::W_SLOTS - 1) * T::W_SLOT ? 0 : w_slot + T::W_SLOT;                 \
+    } else PP_COPY_W()
+    PP_COPY_A_END(0, AC) PP_A_DONE() PP_COPY_W_END()
     if (HP == 2) {
-        PP_COPY_A(0, AC) PP_A_DONE() PP_COPY_W()
+        PP_COPY_A_END(0, AC) PP_A_DONE() PP_COPY_W_END()
     } else {
-        PP_COPY_A(0, AE) PP_COPY_W()
-        PP_COPY_A(AE, AC) PP_A_DONE() PP_COPY_W()
+        PP_COPY_A_END(0, AE) PP_COPY_W_END()
+        PP_COPY_A_END(AE, AC) PP_A_DONE() PP_COPY_W_END()
     }
     PP_WAIT()
     pp_barrier();
@@ -270,31 +299,36 @@ gemm_pp_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
         __builtin_amdgcn_s_setprio(0);                                                                      \
         __builtin_amdgcn_sched_barrier(0);                                                                  \
     }
-#define PP_PHASE(H, LIVE)                                                                                       \
+#define PP_PHASE(H, LIVE, COPY_A, COPY_W)                                                                   \
     {                                                                                                       \
         PP_MEM(H, LIVE)                                                                                      \
-        if (HP == 2) { PP_COPY_A(0, AC) PP_A_DONE() }                                                       \
-        else if ((H) == 0) { PP_COPY_A(0, AE) }                                                             \
-        else { PP_COPY_A(AE, AC) PP_A_DONE() }                                                              \
-        PP_COPY_W()                                                                                         \
+        if (HP == 2) { COPY_A(0, AC) PP_A_DONE() }                                                          \
+        else if ((H) == 0) { COPY_A(0, AE) }                                                                \
+        else { COPY_A(AE, AC) PP_A_DONE() }                                                                 \
+        COPY_W()                                                                                            \
         w_rd = w_rd == (T::W_SLOTS - 1) * T::W_SLOT ? 0 : w_rd + T::W_SLOT;                                 \
         PP_WAIT()                                                                                           \
         pp_barrier();                                                                                       \
         PP_COMPUTE(LIVE)                                                                                      \
         pp_barrier();                                                                                       \
     }
-#define PP_LOOP(LIVE)                                                                                       \
-    for (int s = 0; s < n_steps; ++s) {                                                                     \
-        PP_PHASE(0, LIVE)                                                                                   \
-        if (HP == 1) PP_PHASE(1, LIVE)                                                                      \
+#define PP_LOOP(FROM, TO, LIVE, COPY_A, COPY_W)                                                             \
+    for (int s = FROM; s < (TO); ++s) {                                                                     \
+        PP_PHASE(0, LIVE, COPY_A, COPY_W)                                                                   \
+        if (HP == 1) PP_PHASE(1, LIVE, COPY_A, COPY_W)                                                      \
         a_rd = a_rd == 2 * T::A_STEP ? 0 : a_rd + T::A_STEP;                                                \
     }
-    if (live == RF) { PP_LOOP(RF) } else { PP_LOOP(live) }
+    // (the copies run two steps ahead: up to there they are the product's own)
+    const int n_plain = KIND == EPI_ADAPTERS ? (n_own < 2 ? 0 : n_own - 2) : n_steps;
+    if (live == RF) { PP_LOOP(0, n_plain, RF, PP_COPY_A, PP_COPY_W) } else { PP_LOOP(0, n_plain, live, PP_COPY_A, PP_COPY_W) }
+    if constexpr (KIND == EPI_ADAPTERS) { PP_LOOP(n_plain, n_steps, live, PP_COPY_A_END, PP_COPY_W_END) }
 #undef PP_LOOP
 #undef PP_PHASE
 #undef PP_COMPUTE
 #undef PP_MEM
 #undef PP_WAIT
+#undef PP_COPY_W_END
+#undef PP_COPY_A_END
 #undef PP_COPY_W
 #undef PP_A_DONE
 #undef PP_COPY_A
@@ -302,7 +336,7 @@ gemm_pp_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
     pp_wait<0>();                  // nothing may still be writing LDS when it is used again or the workgroup ends
 
     pp_finish<0, RF, RF, CF, KIND, FP8>(acc, lds_raw, wave, T::PART_FLOATS, n_tile * m_tiles + m_tile, split, splits, partial, arrived,
-                                        M, N, m0_wg + wm * (RF * 16), n0 + wn * (16 * CF), ep);
+                                        M, N, m0_wg + wm * (RF * 16), n0 + wn * (16 * CF), ep, plan);
 }
 
 // Where two groups hold partial sums of the same fragments they exchange halves of them through LDS (see KG_FINISH): rows [I0, I1) of a
@@ -341,8 +375,8 @@ template <int I0, int I1, int RF, int CF> __device__ __forceinline__ void kg_add
             if (kg == 1) kg_add<H, RF>(acc, ex - H * CF * 64);                                              \
         }                                                                                                   \
         if (splits > 1) __syncthreads();   /* the area is read before the arrival flag is written into it */ \
-        if (kg == 0) pp_finish<0, H, RF, CF, KIND, FP8>(acc, lds_raw, w4, T::PART_FLOATS, tile, split, splits, partial, arrived, M, N, m0, n0w, ep); \
-        else pp_finish<H, RF, RF, CF, KIND, FP8>(acc, lds_raw, w4, T::PART_FLOATS, tile, split, splits, partial, arrived, M, N, m0, n0w, ep); \
+        if (kg == 0) pp_finish<0, H, RF, CF, KIND, FP8>(acc, lds_raw, w4, T::PART_FLOATS, tile, split, splits, partial, arrived, M, N, m0, n0w, ep, plan); \
+        else pp_finish<H, RF, RF, CF, KIND, FP8>(acc, lds_raw, w4, T::PART_FLOATS, tile, split, splits, partial, arrived, M, N, m0, n0w, ep, plan); \
     }
 
 // Narrow tiles: the two wave groups take the two 32-k halves of every K-step of the SAME tile, so that a wave of a 128-column
@@ -380,6 +414,13 @@ gemm_kg_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
     const int ks_begin = split * steps_per_split;
     int n_steps = K / 64 - ks_begin;
     n_steps = n_steps < steps_per_split ? n_steps : steps_per_split;
+    // low-rank adapters: their K-steps follow the product's own
+    const int n_own = n_steps;
+    AdapterPlan plan = nullptr;
+    if constexpr (KIND == EPI_ADAPTERS) {
+        plan = adapter_plan(ep.adapters, m_tile);
+        if (split == splits - 1) n_steps += adapter_steps(plan);
+    }
 
     // The copies of a K-step (8 rows of A or one 32-column x 16-k weight block, 1 KiB each) are dealt out to the waves in
     // one list; its end is padded with repetitions of the last copy.
@@ -428,8 +469,28 @@ gemm_kg_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
         _Pragma("unroll") for (int i = 0; i < CW; ++i) pp_copy16(voff[i], base[i] + static_cast<uint64_t>(st_) * stride[i], dst[i] + buf); \
         ++next; buf = buf == (NS - 1) * T::STEP ? 0 : buf + T::STEP;                                        \
     }
-#pragma unroll
-    for (int p = 0; p < NS - 1; ++p) KG_COPY()
+    // the same copies where they may be those of adapters' steps, whose rows come in the order of LDS and whose weights lie where the plan says
+    const char* const t_base = KIND == EPI_ADAPTERS ? adapter_terms(ep.adapters, m_tile) : nullptr;
+#define KG_COPY_END()                                                                                       \
+    if constexpr (KIND == EPI_ADAPTERS) {                                                                   \
+        const int st_ = next < n_steps ? next : n_steps - 1, at_ = st_ - n_own;                             \
+        const AdapterHalf first_ = adapter_half(plan, 2 * (at_ < 0 ? 0 : at_)), second_ = adapter_half(plan, 2 * (at_ < 0 ? 0 : at_) + 1); \
+        _Pragma("unroll") for (int i = 0; i < CW; ++i) {                                                    \
+            int c_ = wave * CW + i;                                                                         \
+            c_ = c_ < T::COPIES ? c_ : T::COPIES - 1;                                                       \
+            const bool rows_ = c_ < T::A_COPIES;                                                            \
+            const int f_ = rows_ ? 0 : c_ - T::A_COPIES;                                                    \
+            int nb_ = (n0 >> 5) + (f_ >> 2);                                                                \
+            nb_ = nb_ < n_blocks ? nb_ : n_blocks - 1;                                                      \
+            const char* const block_ = adapter_block(ep.adapters, {f_ & 2 ? second_.id : first_.id, f_ & 2 ? second_.blocks : first_.blocks}, f_ & 1, nb_); \
+            const char* const theirs_ = rows_ ? t_base + static_cast<int64_t>(at_) * (T::ROWS * 128) + c_ * 1024 : block_; \
+            pp_copy16(at_ >= 0 && rows_ ? static_cast<unsigned>(lane) * 16u : voff[i], at_ >= 0 ? theirs_ : base[i] + static_cast<uint64_t>(st_) * stride[i], dst[i] + buf); \
+            __builtin_amdgcn_sched_barrier(0);   /* one address at a time in scalar registers */            \
+        }                                                                                                   \
+        ++next; buf = buf == (NS - 1) * T::STEP ? 0 : buf + T::STEP;                                        \
+    } else KG_COPY()
+#pragma unroll(KIND == EPI_ADAPTERS ? 1 : NS - 1)
+    for (int p = 0; p < NS - 1; ++p) KG_COPY_END()
     pp_wait<(NS - 2) * CW>();
     pp_barrier();
     if (kg == 1) pp_barrier();     // the second group runs one half phase behind the first
@@ -437,12 +498,12 @@ gemm_kg_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
     bf16x8 af[RF], wf[CF];
     int live = (M - m0_wg - wm * (RF * 16) + 15) >> 4;
     live = live < 0 ? 0 : (live < RF ? live : RF);
-#define KG_LOOP(LIVE)                                                                                       \
-    for (int s = 0; s < n_steps; ++s) {                                                                     \
+#define KG_LOOP(FROM, TO, LIVE, COPY)                                                                                       \
+    for (int s = FROM; s < (TO); ++s) {                                                                     \
         _Pragma("unroll") for (int j = 0; j < CF; ++j) wf[j] = *reinterpret_cast<const bf16x8*>(lds_raw + (w_off[j & 1] + rd) + (j >> 1) * 4096); \
         _Pragma("unroll") for (int i = 0; i < RF; ++i) if (i < (LIVE)) af[i] = *reinterpret_cast<const bf16x8*>(lds_raw + (a_off + rd) + i * 2048); \
         __builtin_amdgcn_sched_barrier(0);                                                                  \
-        KG_COPY()                                                                                           \
+        COPY()                                                                                              \
         rd = rd == (NS - 1) * T::STEP ? 0 : rd + T::STEP;                                                   \
         pp_wait<(NS - 2) * CW>();                                                                           \
         __builtin_amdgcn_sched_barrier(0);                                                                  \
@@ -454,8 +515,12 @@ gemm_kg_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
         __builtin_amdgcn_sched_barrier(0);                                                                  \
         pp_barrier();                                                                                       \
     }
-    if (live == RF) { KG_LOOP(RF) } else { KG_LOOP(live) }
+    // (the copies run NS - 1 steps ahead: up to there they are the product's own)
+    const int n_plain = KIND == EPI_ADAPTERS ? (n_own < NS - 1 ? 0 : n_own - (NS - 1)) : n_steps;
+    if (live == RF) { KG_LOOP(0, n_plain, RF, KG_COPY) } else { KG_LOOP(0, n_plain, live, KG_COPY) }
+    if constexpr (KIND == EPI_ADAPTERS) { KG_LOOP(n_plain, n_steps, live, KG_COPY_END) }
 #undef KG_LOOP
+#undef KG_COPY_END
 #undef KG_COPY
     if (kg == 0) pp_barrier();
     pp_wait<0>();
@@ -583,6 +648,7 @@ gemm_kg8_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict_
     if (kg == 0) pp_barrier();
     pp_wait<0>();
     __syncthreads();
+    constexpr AdapterPlan plan = nullptr;
     KG_FINISH(true)
 }
 

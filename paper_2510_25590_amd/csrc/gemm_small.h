@@ -10,6 +10,7 @@
 #pragma once
 #include "gemm_adapters.h"
 #include "layernorm_row.h"
+#include <type_traits>
 
 namespace {
 
@@ -67,6 +68,8 @@ __device__ __forceinline__ void gemm_small_tile(unsigned char* lds, int tile_y, 
         if (epi_reads<END>()) fin_raw = ep.vec_ok ? epi_load8<END, true>(ep, row, fin_col) : epi_load8<END, false>(ep, row, fin_col);
     }
 
+    typename std::conditional<KIND == EPI_ADAPTERS, AdapterUnits<CF>, char>::type units;
+    if constexpr (KIND == EPI_ADAPTERS) units.fetch(ep.adapters, M, N, m0, n0, wave, kSmallWaves);
     f32x4 acc[CF];
 #pragma unroll
     for (int j = 0; j < CF; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -111,7 +114,7 @@ __device__ __forceinline__ void gemm_small_tile(unsigned char* lds, int tile_y, 
                 for (int j = 0; j < CF; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i][j], a[i], acc[j], 0, 0, 0);
             }
     }
-    if constexpr (KIND == EPI_ADAPTERS) adapters_add<0, 1, 1, CF>(reinterpret_cast<f32x4(&)[1][CF]>(acc), M, N, m0, n0, ep.adapters, wave, kSmallWaves);
+    if constexpr (KIND == EPI_ADAPTERS) units.add(acc, ep.adapters, M, N, m0, n0, kSmallWaves);
     if (LN != LN_NONE) __syncthreads();                         // the rows have been read
     f32x4* sums = reinterpret_cast<f32x4*>(lds) + lane;
 #pragma unroll

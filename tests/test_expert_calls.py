@@ -131,8 +131,7 @@ def test_every_adapter_product_covers_its_result(run):
     for (m, n, k), (code, launches, _, message) in zip(shapes, answers):
         assert code == rg.OK and len(launches) == 2, message
         (dx, dy, _), _, down = launches[0]
-        rows = 16 * int(re.search(r"adapters_down_kernel<(\d+), ", down).group(1))
-        assert dx == -(-m // rows) and dy >= 1
+        assert dx == -(-m // 16) and dy >= 1
         (x, y, _), lds, kernel = launches[1]
         kind, numbers = re.search(r"gemm_(small|pp|kg)_kernel<([\d, a-z]+)>", kernel).groups()
         args = [int(v) for v in re.findall(r"\d+", numbers)]
@@ -145,13 +144,17 @@ def test_every_adapter_product_covers_its_result(run):
             assert x >= -(-m // tile[0]) * -(-n // tile[1]) and y == 1
     assert {s[0] for s in seen} == {"small", "pp", "kg"}
     many = run([BF, adapters(m=2000, n=64, k=64, rank=256, sel=32, out=1)])[1]
-    assert len(many[1]) == 2 * 4                                         # 512 rows at a time
+    assert len(many[1]) == 2 * 3                                         # 672 rows at a time
+    # where every row of a tile may name another adapter: passes of as many tiles as the workspace holds, or, below 1024 rows, the kernel of 16 rows
+    passes, single = run([BF, adapters(m=4200, n=2304, k=128, rank=8, count=600), adapters(m=4200, n=2304, k=128, rank=8, count=5000, sel=4)])[1:]
+    assert len(passes[1]) > 2 and len(passes[1]) % 2 == 0 and all(re.search("gemm_(pp|kg)", kernel) for _, _, kernel in passes[1][1::2])
+    assert len(single[1]) == 2 and "gemm_small" in single[1][1][2]
 
 
 @pytest.mark.parametrize("rows,cols,rank", [(1, 64, 1), (33, 128, 16), (9216, 3072, 64), (40, 64, 17)])
 def test_tensor_sizes(rows, cols, rank):
     r16, n32 = -(-rank // 16) * 16, -(-rows // 32) * 32
-    assert rg.regione_packed_adapter_elems(rows, cols, rank) == r16 * cols + n32 * r16
+    assert rg.regione_packed_adapter_elems(rows, cols, rank) == r16 * cols + n32 * r16 + -(-(n32 // 32 + 1) // 4) * 8
     assert rg.regione_packed_adapter_elems(0, cols, rank) == rg.regione_packed_adapter_elems(rows, 0, rank) == rg.regione_packed_adapter_elems(rows, cols, 0) == 0
 
 

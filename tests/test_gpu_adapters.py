@@ -147,12 +147,30 @@ def test_rows_without_adapters_are_the_plain_product(ctx, m, n):
 
 
 def test_more_inner_products_than_are_kept_at_a_time(ctx):
-    """32 adapters of rank 256 per row, float32: 512 rows at a time."""
+    """32 adapters of rank 256 per row, float32: 672 rows at a time."""
     o = Operands(ctx, 1100, 64, 64, 256, 40, 32, "router", 7, True)
     o.which[:, 8:] = -1                                                  # (the reference's time)
     o.which[:, 31] = 39
     o.whichd = up(o.which)
     assert np.array_equal(o.call(ctx, torch.empty(1100, 64, device="cuda")).cpu().double().numpy(), o.reference()[0])
+
+
+@pytest.mark.parametrize("count,sel", [(600, 1), (5000, 4)])
+def test_many_adapters_in_a_tile(ctx, count, sel):
+    """Tiles that may name more adapters than the workspace has room for: passes over the rows; and the kernel of 16 rows."""
+    m, n, k = 4200, 2304, 128
+    o = Operands(ctx, m, n, k, 8, 8, sel, "router", 8, True)
+    rng = np.random.default_rng(3)
+    ids = np.sort(rng.choice(count, 8, replace=False))
+    packed = torch.zeros(count, o.ap.shape[1], dtype=torch.bfloat16, device="cuda")
+    packed[torch.from_numpy(ids).cuda()] = o.ap
+    which = ids[o.which]
+    which[::7] = rng.integers(0, count, which[::7].shape)                # adapters of zeros, but for the eight
+    o.ap, o.whichd, o.count = packed, up(which.astype(np.int32)), count
+    at = np.searchsorted(ids, which).clip(0, 7)
+    o.which = np.where(ids[at] == which, at, -1).astype(np.int32)
+    y = o.call(ctx, torch.full((m, n), 7.0, device="cuda"))
+    assert np.array_equal(y.cpu().double().numpy(), o.reference()[0])
 
 
 def test_adapters_past_32_bits(ctx):
