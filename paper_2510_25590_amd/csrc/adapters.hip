@@ -138,28 +138,50 @@ adapters_down_rows_kernel(DownCall d) {
     put_terms([&](int c) { return row + c; }, kc, block, d.blocks, d.terms, d.cols, w, acc);
 }
 
-// For tiles (their layout and plan: gemm_adapters.h): a workgroup owns 16 rows and goes through the blocks of 16 ranks of their adapters, NB at a time; those of the tile that none of the rows
-// names are zeros there.  Workgroups of the same rows (blockIdx.y) take turns.  WAVES waves split K and meet in LDS, where the sums are formed in wave order.
+// For tiles (their layout and plan: gemm_adapters.h): a workgroup owns 16 * RB rows and goes through the blocks of 16 ranks of their adapters, NB at a time; those of the tile that none of the
+// rows names are zeros there.  Workgroups of the same rows (blockIdx.y) take turns.  WAVES waves split K and meet in LDS, where the sums are formed in wave order.
+// The rows come in whole lines, 8 x 128 bytes to a load, and change to fragments in a part of LDS that is the wave's own.  What bounds it is the way from L2 into a CU, 20 bytes a cycle: all of A
+// for every workgroup beside its rows, so that 32 rows to a workgroup pay where there are workgroups enough.  8704 rows, K 3072, rank 64: 24 us (33 with x from HBM), 6 of them the launch and the list of the
+// adapters; with A from L1 20, with x from L1 too 18.  As fragments from memory, 64 bytes of 16 rows to a load, x took half as long again.
+// Steps past a wave's own are multiplied with zeros: a branch around the products lets the compiler move the loads into it, behind all that should hide them.
 struct DownTiles { int rows, plan_pitch; int64_t tile_elems; int32_t* plan; int64_t bad; };      // rows of a tile; elements of an adapter ahead of its bits
-template <int NB, int WAVES>
+template <int RB, int NB, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64)
 adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
-    constexpr int AHEAD = 4, T = WAVES * 64;
-    __shared__ uint32_t named[2][kMostAdapters / 32];             // by the tile, by the 16 rows
-    __shared__ int32_t ids[16 * kMostSel];
-    __shared__ float weights[16 * kMostSel];
-    __shared__ __attribute__((aligned(16))) f32x4 sums[WAVES][NB][64];
+    constexpr int T = WAVES * 64, ROWS = 16 * RB, AHEAD = 2;
+    __shared__ uint32_t named[2][kMostAdapters / 32];             // by the tile, by the workgroup's rows
+    __shared__ int32_t ids[ROWS * kMostSel];
+    __shared__ float weights[ROWS * kMostSel];
+    // a wave's rows of a step on their way from whole lines to fragments; at the end the sums
+    constexpr int TURN = 2048 * RB, SUMS = NB * 1024;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[WAVES * (TURN > SUMS ? TURN : SUMS)];
+    static_assert(NB <= WAVES && sizeof(named) + sizeof(ids) + sizeof(weights) + sizeof(lds) <= 65536, "a wave per block at the end, and LDS");
+    unsigned char (*const turn)[TURN] = reinterpret_cast<unsigned char (*)[TURN]>(lds);
+    f32x4 (*const sums)[NB][64] = reinterpret_cast<f32x4 (*)[NB][64]>(lds);
     const int lane = threadIdx.x & 63, l16 = lane & 15, kc = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int m0 = blockIdx.x * 16, rows = d.m - m0 < 16 ? d.m - m0 : 16;
-    const int tile = m0 / tiles.rows, t0 = tile * tiles.rows, tile_rows = d.m - t0 < tiles.rows ? d.m - t0 : tiles.rows;
-    const int steps = d.k >> 5, per = (steps + WAVES - 1) / WAVES, s0 = wave * per;
+    const int pieces = (tiles.rows + ROWS - 1) / ROWS, tile = blockIdx.x / pieces, row0 = (blockIdx.x - tile * pieces) * ROWS;
+    const int t0 = tile * tiles.rows, tile_rows = d.m - t0 < tiles.rows ? d.m - t0 : tiles.rows, m0 = t0 + row0;
+    const int rows = tile_rows - row0 < ROWS ? tile_rows - row0 : ROWS, place_rows = tiles.rows - row0 < ROWS ? tiles.rows - row0 : ROWS;
+    if (rows <= 0) return;                                        // (the last tile's end)
+    const int steps = d.k >> 6, per = (steps + WAVES - 1) / WAVES, s0 = wave * per;        // of 64 inputs
     const int own = s0 + per < steps ? per : (steps > s0 ? steps - s0 : 0);
-    const bf16_t* const xp = d.x + static_cast<int64_t>(m0 + (l16 < rows ? l16 : rows - 1)) * d.k + 8 * kc;        // rows past the end repeat the last one
-    bf16x8 xf[AHEAD], wf[AHEAD][NB];
+    const bf16_t* xp[2 * RB];
+#pragma unroll
+    for (int i = 0; i < 2 * RB; ++i) {
+        const int row = 8 * i + (lane >> 3);
+        xp[i] = d.x + static_cast<int64_t>(m0 + (row < rows ? row : rows - 1)) * d.k + 8 * (lane & 7);      // rows past the end repeat the last one
+    }
+    u32x4 xr[AHEAD][2 * RB];
+    bf16x8 wf[AHEAD][2][NB];
+    unsigned char* const put = turn[wave] + (lane >> 3) * 128 + (((lane & 7) ^ ((lane >> 4) & 3)) << 4);
+    unsigned char* const put_odd = turn[wave] + (lane >> 3) * 128 + (((lane & 7) ^ (((lane >> 4) & 3) + 4)) << 4);       // rows 8 on of 16
+    const unsigned char* const get = turn[wave] + l16 * 128;
     auto step_of = [&](int c) __attribute__((always_inline)) { const int s = s0 + c; return s < steps ? s : steps - 1; };      // (what is past the wave's steps is not multiplied)
 #pragma unroll
-    for (int c = 0; c < AHEAD; ++c) xf[c] = *reinterpret_cast<const bf16x8*>(xp + step_of(c) * 32);
+    for (int c = 0; c < AHEAD; ++c)
+#pragma unroll
+        for (int i = 0; i < 2 * RB; ++i) xr[c][i] = *reinterpret_cast<const u32x4*>(xp[i] + step_of(c) * 64);
 
     const int words = (d.count + 31) / 32;
     for (int i = threadIdx.x; i < words; i += T) named[0][i] = named[1][i] = 0u;
@@ -182,11 +204,12 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
     auto place = [&](int row, int half, int c) __attribute__((always_inline)) {       // term c of a half of a step, in the order of LDS
         return t + (static_cast<int64_t>(half >> 1) * tiles.rows + row) * 128 + ((((half & 1) * 4 + (c >> 3)) ^ ((row >> 1) & 7)) << 4) + (c & 7) * 2;
     };
-    const int halves = d.cols >> 5, row0 = m0 - t0;
-    const bool lead = m0 == t0 && blockIdx.y == 0;
+    const int halves = d.cols >> 5;
+    const bool lead = row0 == 0 && blockIdx.y == 0;
     int32_t* const plan = tiles.plan + static_cast<int64_t>(tile) * tiles.plan_pitch;
     auto zeros = [&](int half, int count) __attribute__((always_inline)) {
-        for (int i = threadIdx.x; i < count * 64; i += T) *reinterpret_cast<uint4*>(place(row0 + (i >> 2 & 15), half + (i >> 6), (i & 3) * 8)) = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = threadIdx.x; i < count * (ROWS * 4); i += T)
+            if (i / 4 % ROWS < place_rows) *reinterpret_cast<uint4*>(place(row0 + i / 4 % ROWS, half + i / (ROWS * 4), (i & 3) * 8)) = make_uint4(0u, 0u, 0u, 0u);
     };
 
     int a = -1, pos = -1, block = d.blocks;
@@ -234,47 +257,72 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
         if (units == 0 || batch % gridDim.y != blockIdx.y) continue;
         const bf16_t* wp[NB];
 #pragma unroll
-        for (int q = 0; q < NB; ++q) wp[q] = d.packed + static_cast<int64_t>(q < units ? unit_a[q] : unit_a[0]) * d.stride + static_cast<int64_t>(q < units ? unit_block[q] : unit_block[0]) * steps * 512 + lane * 8;
-        f32x4 acc[NB];
+        for (int q = 0; q < NB; ++q) wp[q] = d.packed + static_cast<int64_t>(q < units ? unit_a[q] : unit_a[0]) * d.stride + static_cast<int64_t>(q < units ? unit_block[q] : unit_block[0]) * steps * 1024 + lane * 8;
+        f32x4 acc[RB][NB];
 #pragma unroll
-        for (int q = 0; q < NB; ++q) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int q = 0; q < NB; ++q) acc[i][q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < AHEAD; ++c) {
             const int s = step_of(c);
-            if (!first_batch) xf[c] = *reinterpret_cast<const bf16x8*>(xp + s * 32);
+            if (!first_batch)
 #pragma unroll
-            for (int q = 0; q < NB; ++q) wf[c][q] = *reinterpret_cast<const bf16x8*>(wp[q] + static_cast<int64_t>(s) * 512);
+                for (int i = 0; i < 2 * RB; ++i) xr[c][i] = *reinterpret_cast<const u32x4*>(xp[i] + s * 64);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int q = 0; q < NB; ++q) wf[c][h][q] = *reinterpret_cast<const bf16x8*>(wp[q] + static_cast<int64_t>(s) * 1024 + h * 512);
         }
         first_batch = false;
         for (int base = 0; base < own; base += AHEAD)
 #pragma unroll
             for (int c = 0; c < AHEAD; ++c) {
-                if (base + c < own)
 #pragma unroll
-                    for (int q = 0; q < NB; ++q) acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[c][q], xf[c], acc[q], 0, 0, 0);
+                for (int i = 0; i < 2 * RB; ++i) *reinterpret_cast<u32x4*>(i & 1 ? put_odd + i * 1024 : put + i * 1024) = base + c < own ? xr[c][i] : u32x4{0u, 0u, 0u, 0u};
                 const int s = step_of(base + c + AHEAD);
-                xf[c] = *reinterpret_cast<const bf16x8*>(xp + s * 32);
 #pragma unroll
-                for (int q = 0; q < NB; ++q) wf[c][q] = *reinterpret_cast<const bf16x8*>(wp[q] + static_cast<int64_t>(s) * 512);
+                for (int i = 0; i < 2 * RB; ++i) xr[c][i] = *reinterpret_cast<const u32x4*>(xp[i] + s * 64);
+                bf16x8 xf[2][RB];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < RB; ++i) xf[h][i] = *reinterpret_cast<const bf16x8*>(get + i * 2048 + (((4 * h + kc) ^ (l16 >> 1)) << 4));
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int q = 0; q < NB; ++q)
+#pragma unroll
+                        for (int i = 0; i < RB; ++i) acc[i][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[c][h][q], xf[h][i], acc[i][q], 0, 0, 0);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int q = 0; q < NB; ++q) wf[c][h][q] = *reinterpret_cast<const bf16x8*>(wp[q] + static_cast<int64_t>(s) * 1024 + h * 512);
+                __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-        for (int q = 0; q < NB; ++q) sums[wave][q][lane] = acc[q];
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < NB; ++q)
-            if (q % WAVES == wave && q < units) {
-                f32x4 sum = sums[0][q][lane];
+        for (int i = 0; i < RB; ++i) {
 #pragma unroll
-                for (int v = 1; v < WAVES; ++v) sum += sums[v][q][lane];
-                bool its = false;
-                float w = 0.f;
-                if (l16 < rows)
-                    for (int s = d.sel - 1; s >= 0; --s)
-                        if (ids[l16 * d.sel + s] == unit_a[q]) { its = true; w += weights[l16 * d.sel + s]; }
-                const int half0 = unit_pos[q] * halves;
-                put_terms([&](int c) { return place(row0 + l16, half0 + (c >> 5), c & 31); }, kc, unit_block[q], d.blocks, d.terms, d.cols, w, sum, its);
-            }
-        __syncthreads();
+            for (int q = 0; q < NB; ++q) sums[wave][q][lane] = acc[i][q];
+            __syncthreads();
+#pragma unroll
+            for (int q = 0; q < NB; ++q)
+                if (q == wave && q < units) {
+                    f32x4 sum = sums[0][q][lane];
+#pragma unroll
+                    for (int v = 1; v < WAVES; ++v) sum += sums[v][q][lane];
+                    const int row = 16 * i + l16, half0 = unit_pos[q] * halves;
+                    bool its = false;
+                    float w = 0.f;
+                    if (row < rows)
+                        for (int s = d.sel - 1; s >= 0; --s)
+                            if (ids[row * d.sel + s] == unit_a[q]) { its = true; w += weights[row * d.sel + s]; }
+                    if (row < place_rows) put_terms([&](int c) { return place(row0 + row, half0 + (c >> 5), c & 31); }, kc, unit_block[q], d.blocks, d.terms, d.cols, w, sum, its);
+                }
+            __syncthreads();
+        }
     }
     const int all = (pos + 1) * halves;
     if ((all & 1) && blockIdx.y == 0) zeros(all, 1);              // the last step's second half
@@ -291,17 +339,20 @@ int down_rows(regione_ctx* ctx, const DownCall& d) {
     return REGIONE_OK;
 }
 
-constexpr int kDownFew = 128;                                    // pieces of 16 rows up to which every block of ranks has workgroups of its own
+template <int RB, int NB, int WAVES>
+void launch_down_tiles(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
+    const int pieces = (d.m + tiles.rows - 1) / tiles.rows * ((tiles.rows + 16 * RB - 1) / (16 * RB));
+    const int64_t most = static_cast<int64_t>(16 * RB) * d.sel < d.count ? static_cast<int64_t>(16 * RB) * d.sel : d.count, batches = (most * d.blocks + NB - 1) / NB;
+    const int64_t room = pieces < 512 ? 512 / pieces : 1;
+    hipLaunchKernelGGL((adapters_down_tiles_kernel<RB, NB, WAVES>), dim3(pieces, static_cast<unsigned>(batches < room ? batches : room)), dim3(WAVES * 64), 0, ctx->stream, d, tiles);
+}
 int down_tiles(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
-    const int pieces = (d.m + 15) / 16;
-    const int64_t most = static_cast<int64_t>(16) * d.sel < d.count ? static_cast<int64_t>(16) * d.sel : d.count, units = most * d.blocks;      // of 16 rows
-    const int64_t room = pieces < 1024 ? 1024 / pieces : 1;
-    if (pieces <= kDownFew) {
-        hipLaunchKernelGGL((adapters_down_tiles_kernel<1, 8>), dim3(pieces, static_cast<unsigned>(units < room ? units : room)), dim3(512), 0, ctx->stream, d, tiles);
-    } else {
-        const int64_t batches = (units + 3) / 4;
-        hipLaunchKernelGGL((adapters_down_tiles_kernel<4, 4>), dim3(pieces, static_cast<unsigned>(batches < room ? batches : room)), dim3(256), 0, ctx->stream, d, tiles);
-    }
+    // us, K 3072, a block of ranks to a workgroup / four / four of 32 rows: 820 rows, rank 16 6.5 / 8.2 / 10.1, rank 64 10.9 / 10.3 / 12.3; 2048 rows, rank 16 6.8 / 8.2 / 9.8, rank 64
+    // 12.6 / 10.5 / 12.1; 4096 rows, rank 16 10.8 / 9.1 / 10.4, rank 64 18.1 / 12.1 / 12.7; 6144 rows, rank 64 24.9 / 16.8 / 14.8; 8704 rows, rank 64 46 / 24.7 / 24.4; 16384 rows 68 / 43 / 34
+    const int64_t pieces = (d.m + 15) / 16, units = pieces * d.blocks * (d.sel < d.count ? d.sel : d.count);
+    if (units <= 192) launch_down_tiles<1, 1, 8>(ctx, d, tiles);
+    else if (pieces <= 256) launch_down_tiles<1, 4, 4>(ctx, d, tiles);
+    else launch_down_tiles<2, 4, 4>(ctx, d, tiles);
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }

@@ -131,17 +131,19 @@ def test_every_adapter_product_covers_its_result(run):
     for (m, n, k), (code, launches, _, message) in zip(shapes, answers):
         assert code == rg.OK and len(launches) == 2, message
         (dx, dy, _), _, down = launches[0]
-        assert dx == -(-m // 16) and dy >= 1
         (x, y, _), lds, kernel = launches[1]
         kind, numbers = re.search(r"gemm_(small|pp|kg)_kernel<([\d, a-z]+)>", kernel).groups()
         args = [int(v) for v in re.findall(r"\d+", numbers)]
         seen.add((kind,) + tuple(args))
         assert lds <= 163840
         if kind == "small":
+            assert "adapters_down_rows" in down and dx == -(-m // 16) and dy >= 1
             assert x == -(-n // (16 * args[0])) and y == -(-m // 16)
         else:
             tile = (32 * args[0], 64 * args[1]) if kind == "pp" else (16 * args[0] * args[2], 16 * args[1] * (4 // args[2]))
             assert x >= -(-m // tile[0]) * -(-n // tile[1]) and y == 1
+            rows = 16 * int(re.search(r"adapters_down_tiles_kernel<(\d+), ", down).group(1))
+            assert dx == -(-m // tile[0]) * -(-tile[0] // rows) and dy >= 1
     assert {s[0] for s in seen} == {"small", "pp", "kg"}
     many = run([BF, adapters(m=2000, n=64, k=64, rank=256, sel=32, out=1)])[1]
     assert len(many[1]) == 2 * 3                                         # 672 rows at a time
