@@ -164,8 +164,8 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
     const int t0 = tile * tiles.rows, tile_rows = d.m - t0 < tiles.rows ? d.m - t0 : tiles.rows, m0 = t0 + row0;
     const int rows = tile_rows - row0 < ROWS ? tile_rows - row0 : ROWS, place_rows = tiles.rows - row0 < ROWS ? tiles.rows - row0 : ROWS;
     if (rows <= 0) return;                                        // (the last tile's end)
-    const int steps = d.k >> 6, per = (steps + WAVES - 1) / WAVES, s0 = wave * per;        // of 64 inputs
-    const int own = s0 + per < steps ? per : (steps > s0 ? steps - s0 : 0);
+    const int steps = d.k >> 6, share = (steps + WAVES - 1) / WAVES, s0 = wave * share;    // of 64 inputs
+    const int own = s0 + share < steps ? share : (steps > s0 ? steps - s0 : 0);
     const bf16_t* xp[2 * RB];
 #pragma unroll
     for (int i = 0; i < 2 * RB; ++i) {
@@ -201,18 +201,20 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
     __syncthreads();
 
     unsigned char* const t = reinterpret_cast<unsigned char*>(d.t + tile * tiles.tile_elems);
-    auto place = [&](int row, int half, int c) __attribute__((always_inline)) {       // term c of a half of a step, in the order of LDS
-        return t + (static_cast<int64_t>(half >> 1) * tiles.rows + row) * 128 + ((((half & 1) * 4 + (c >> 3)) ^ ((row >> 1) & 7)) << 4) + (c & 7) * 2;
+    auto place = [&](int row, int of, int c) __attribute__((always_inline)) {       // column c of a block of 16 terms, in the order of LDS
+        return t + (static_cast<int64_t>(of >> 2) * tiles.rows + row) * 128 + ((((of & 3) * 2 + (c >> 3)) ^ ((row >> 1) & 7)) << 4) + (c & 7) * 2;
     };
-    const int halves = d.cols >> 5;
+    const int per = d.terms * d.blocks;                           // blocks of 16 terms of an adapter
     const bool lead = row0 == 0 && blockIdx.y == 0;
     int32_t* const plan = tiles.plan + static_cast<int64_t>(tile) * tiles.plan_pitch;
-    auto zeros = [&](int half, int count) __attribute__((always_inline)) {
-        for (int i = threadIdx.x; i < count * (ROWS * 4); i += T)
-            if (i / 4 % ROWS < place_rows) *reinterpret_cast<uint4*>(place(row0 + i / 4 % ROWS, half + i / (ROWS * 4), (i & 3) * 8)) = make_uint4(0u, 0u, 0u, 0u);
+    int64_t* const offsets = reinterpret_cast<int64_t*>(plan + 4);
+    const int ids_at = 4 + (tiles.plan_pitch - 4) / 3 * 2;
+    auto zeros = [&](int of, int count) __attribute__((always_inline)) {
+        for (int i = threadIdx.x; i < count * (ROWS * 2); i += T)
+            if (i / 2 % ROWS < place_rows) *reinterpret_cast<uint4*>(place(row0 + i / 2 % ROWS, of + i / (ROWS * 2), (i & 1) * 8)) = make_uint4(0u, 0u, 0u, 0u);
     };
 
-    int a = -1, pos = -1, block = d.blocks;
+    int a = -1, last = 0, pos = -1, block = d.blocks;
     bool in_rows = false;
     uint32_t bad = 0;
     auto next_adapter = [&]() __attribute__((always_inline)) {    // the tile's next one, in order
@@ -234,16 +236,16 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
         }
         if (a == kNoAdapter) return;
         ++pos;
+        last = a;
         in_rows = named[1][a >> 5] >> (a & 31) & 1u;
         if (lead) {
-            for (int i = threadIdx.x; i < halves; i += T) {
-                const int first = 2 * i % d.blocks, second = (2 * i + 1) % d.blocks;
-                plan[2 + 2 * (pos * halves + i)] = a;
-                plan[3 + 2 * (pos * halves + i)] = first | second << 16;
+            for (int i = threadIdx.x; i < per; i += T) {
+                offsets[pos * per + i] = (a * d.stride + (i % d.blocks) * 512) * 2;
+                plan[ids_at + pos * per + i] = a;
             }
             if (threadIdx.x == 0) bad |= *reinterpret_cast<const uint32_t*>(d.packed + static_cast<int64_t>(a) * d.stride + tiles.bad);
         }
-        if (!in_rows && pos % gridDim.y == blockIdx.y) zeros(pos * halves, halves);
+        if (!in_rows && pos % gridDim.y == blockIdx.y) zeros(pos * per, per);
     };
     bool first_batch = true;
     for (unsigned batch = 0; a != kNoAdapter; ++batch) {
@@ -313,23 +315,24 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
                     f32x4 sum = sums[0][q][lane];
 #pragma unroll
                     for (int v = 1; v < WAVES; ++v) sum += sums[v][q][lane];
-                    const int row = 16 * i + l16, half0 = unit_pos[q] * halves;
+                    const int row = 16 * i + l16, first = unit_pos[q] * per;
                     bool its = false;
                     float w = 0.f;
                     if (row < rows)
                         for (int s = d.sel - 1; s >= 0; --s)
                             if (ids[row * d.sel + s] == unit_a[q]) { its = true; w += weights[row * d.sel + s]; }
-                    if (row < place_rows) put_terms([&](int c) { return place(row0 + row, half0 + (c >> 5), c & 31); }, kc, unit_block[q], d.blocks, d.terms, d.cols, w, sum, its);
+                    if (row < place_rows) put_terms([&](int c) { return place(row0 + row, first + (c >> 4), c & 15); }, kc, unit_block[q], d.blocks, d.terms, 0, w, sum, its);
                 }
             __syncthreads();
         }
     }
-    const int all = (pos + 1) * halves;
-    if ((all & 1) && blockIdx.y == 0) zeros(all, 1);              // the last step's second half
+    const int all = (pos + 1) * per, filled = (all + 3) & ~3;     // whole steps
+    if (filled > all && blockIdx.y == 0) zeros(all, filled - all);
     if (lead && threadIdx.x == 0) {
-        plan[0] = all;
+        plan[0] = filled / 4;
         plan[1] = static_cast<int32_t>(bad);
-        if (all & 1) { plan[2 + 2 * all] = plan[2 + 2 * (all - 1)]; plan[3 + 2 * all] = 0; }
+        plan[2] = ids_at;
+        for (int i = all; i < filled; ++i) { offsets[i] = last * d.stride * 2; plan[ids_at + i] = last; }
     }
 }
 
@@ -414,8 +417,8 @@ extern "C" int regione_linear_adapters(regione_ctx* ctx, const void* x, const vo
     ctx->gemm_part_bytes = all - room;
     AdapterTiles tiles = rg_adapter_tiles(ctx, m, n, k);
     // the most that a tile can name: every row another adapter
-    const int64_t named = static_cast<int64_t>(tiles.rows) * n_sel < n_adapters ? static_cast<int64_t>(tiles.rows) * n_sel : n_adapters, tile_steps = (named * (cols / 32) + 1) / 2;
-    const int64_t tile_bytes = tile_steps * tiles.rows * 128, plan_bytes = (2 + 4 * tile_steps) * 4, fits = static_cast<int64_t>(room) / (tile_bytes + plan_bytes), m_tiles = (m + tiles.rows - 1) / tiles.rows;
+    const int64_t named = static_cast<int64_t>(tiles.rows) * n_sel < n_adapters ? static_cast<int64_t>(tiles.rows) * n_sel : n_adapters, tile_steps = (named * terms * blocks + 3) / 4;
+    const int64_t tile_bytes = tile_steps * tiles.rows * 128, plan_words = 4 + 12 * tile_steps, plan_bytes = plan_words * 4, fits = static_cast<int64_t>(room) / (tile_bytes + plan_bytes), m_tiles = (m + tiles.rows - 1) / tiles.rows;
     int64_t chunk = m;
     if (tiles.tile && fits < m_tiles) {
         if (fits * tiles.rows >= kLeastChunk) {
@@ -447,7 +450,7 @@ extern "C" int regione_linear_adapters(regione_ctx* ctx, const void* x, const vo
         ep.adapters = {d.t, d.which, b, reinterpret_cast<const uint32_t*>(b + b_elems(n, blocks)), d.stride, n_sel, n_adapters, cols, blocks, nullptr, 0, 0};
         if (tiles.tile) {
             const int64_t parts = (rows + tiles.rows - 1) / tiles.rows;
-            DownTiles at = {tiles.rows, static_cast<int>(2 + 4 * tile_steps), tile_bytes / 2, reinterpret_cast<int32_t*>(end + parts * tile_bytes), a_elems(k, blocks) + b_elems(n, blocks) + 2 * ((static_cast<int64_t>(n) + 31) / 32)};
+            DownTiles at = {tiles.rows, static_cast<int>(plan_words), tile_bytes / 2, reinterpret_cast<int32_t*>(end + parts * tile_bytes), a_elems(k, blocks) + b_elems(n, blocks) + 2 * ((static_cast<int64_t>(n) + 31) / 32)};
             ep.adapters.plan = at.plan; ep.adapters.plan_pitch = at.plan_pitch; ep.adapters.tile_elems = at.tile_elems;
             rc = down_tiles(ctx, d, at);
         } else {

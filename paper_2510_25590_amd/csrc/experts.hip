@@ -9,7 +9,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMostExperts = 1024, kMostChosen = 32, kMostGroups = 64;
 constexpr int64_t kMostPairs = int64_t{1} << 24;             // rows that a grouped product takes
-constexpr int64_t kRouteShared = 16384;                      // tokens from which on four share a wave
+// Tokens from which on four share a wave, without and with scores to look at beside the logits (bias, groups).  us, a wave to a token / to four: 64 experts, float32, 6 chosen, 1024 tokens 3.7 / 3.6, 4608
+// 4.9 / 4.0, 65536 27.5 / 11.3; 256 experts, bf16, 8 chosen, 1024 tokens 4.7 / 5.0, 2048 5.2 / 5.1, 65536 46 / 21; 256 experts in 8 groups with a bias, 8 chosen, 1024 tokens 7.0 / 9.0, 4608 10.9 / 11.4,
+// 8192 14.5 / 12.5, 65536 79 / 50
+constexpr int64_t kRouteShared = 2048, kRouteSharedScored = 8192;
 
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -556,7 +559,7 @@ int launch_route(regione_ctx* ctx, RouteCall& c, bool scored) {
 template <typename T>
 int launch_route(regione_ctx* ctx, RouteCall& c, bool scored) {
     // (two lanes more than choices)
-    if (c.n_tokens >= kRouteShared && c.top_k <= 14 && c.n_groups <= 16) {
+    if (c.n_tokens >= (scored ? kRouteSharedScored : kRouteShared) && c.top_k <= 14 && c.n_groups <= 16) {
         const int need = experts_per_lane(c, 16);
         if (need <= 4) return launch_route<T, 16, 4>(ctx, c, scored);
         if (need <= 8) return launch_route<T, 16, 8>(ctx, c, scored);

@@ -5,8 +5,8 @@
 // projection's sums: nothing is written or read in between, and the result is rounded once.
 //
 // Tiles (gemm_pp.h) take the terms as K-steps behind the product's own: for every adapter that a row of the tile names, in ascending order, its terms in all of the tile's rows, zeros in those
-// that do not name it, in the order that a step has in LDS, the tile's steps one after the other.  The plan of a tile: the number of its halves of steps (32 terms), whether one of its
-// adapters has values in B that are not finite, and for each half the adapter and the two blocks of 16 ranks of B that it meets.  As steps of the same loop they cost what K costs, and their
+// that do not name it, in the order that a step has in LDS, the tile's steps one after the other.  The plan of a tile, 32-bit words: the number of its steps, whether one of its
+// adapters has values in B that are not finite, where the adapters stand, one unused; for each 16 terms where the block of 16 ranks of B that they meet begins (64 bits), and for each 16 terms the adapter.  As steps of the same loop they cost what K costs, and their
 // first loads fly under the product's last steps.  Summed at the end of the tile, each wave its rows and their adapters, they waited for memory step by step, 1.7 us each.
 // Rows without the adapter must not see its values (zero times infinity): what is not finite in B is zero in the packed adapter, and the columns that hold such values are spoilt at the end,
 // in the rows that name the adapter.
@@ -16,15 +16,16 @@
 namespace {
 
 typedef const __attribute__((address_space(4))) int32_t* AdapterPlan;          // read by the scalar unit: no vector load among the counted copies
+typedef __attribute__((ext_vector_type(4), aligned(8))) int64_t AdapterStep;     // where a step's four blocks of B begin, in bytes from `b`
 __device__ __forceinline__ AdapterPlan adapter_plan(const AdapterRows& ad, int tile) { return (AdapterPlan)(ad.plan + static_cast<int64_t>(tile) * ad.plan_pitch); }
-__device__ __forceinline__ int adapter_steps(AdapterPlan plan) { return (plan[0] + 1) >> 1; }
+__device__ __forceinline__ int adapter_steps(AdapterPlan plan) { return plan[0]; }
+// (a tile without adapters reads what its plan's memory holds; no copy goes there)
+__device__ __forceinline__ AdapterStep adapter_step(AdapterPlan plan, int at) { return reinterpret_cast<const __attribute__((address_space(4))) AdapterStep*>(plan + 4)[at]; }
 __device__ __forceinline__ const char* adapter_terms(const AdapterRows& ad, int tile) { return reinterpret_cast<const char*>(ad.t + tile * ad.tile_elems); }
-// a half of a step: its adapter and the two blocks of 16 ranks of B that its terms meet
-struct AdapterHalf { int id, blocks; };
-__device__ __forceinline__ AdapterHalf adapter_half(AdapterPlan plan, int half) { return {plan[2 + 2 * half], plan[3 + 2 * half]}; }
-// 32 columns x 16 ranks of B: block j of the half, column block nb
-__device__ __forceinline__ const char* adapter_block(const AdapterRows& ad, const AdapterHalf& half, int j, int nb) {
-    return reinterpret_cast<const char*>(ad.b + half.id * ad.stride + (static_cast<int64_t>(nb) * ad.blocks + (j ? half.blocks >> 16 : half.blocks & 0xffff)) * 512);
+// 32 columns x 16 ranks of B: block j of a step in column block nb
+__device__ __forceinline__ const char* adapter_block(const AdapterRows& ad, const AdapterStep& step, int j, int nb) {
+    const int64_t low = j & 1 ? step[1] : step[0], high = j & 1 ? step[3] : step[2];
+    return reinterpret_cast<const char*>(ad.b) + (j & 2 ? high : low) + static_cast<int64_t>(nb) * (ad.blocks * 1024);
 }
 // the bits of 32 columns of an adapter
 __device__ __forceinline__ uint32_t adapter_bad(const AdapterRows& ad, int id, int nb) { return ad.bad[(static_cast<int64_t>(id) * ad.stride >> 1) + nb]; }
@@ -32,11 +33,12 @@ __device__ __forceinline__ uint32_t adapter_bad(const AdapterRows& ad, int id, i
 // Rows [I0, I1) of a wave's fragments, in the layout of gemm_epilogue16: columns of adapters that hold values that are not finite, in the rows that name the adapter.
 template <int I0, int I1, int RF, int CF> __device__ __forceinline__ void adapters_spoil(f32x4 (&acc)[RF][CF], int M, int N, int m0, int n0w, const AdapterRows& ad, AdapterPlan plan) {
     if (plan[1] == 0) return;
-    const int lane = threadIdx.x & 63, last_block = ((N + 31) >> 5) - 1, halves = plan[0];
+    const int lane = threadIdx.x & 63, last_block = ((N + 31) >> 5) - 1, blocks = 4 * plan[0];
+    const AdapterPlan ids = plan + plan[2];
     int last = -1;
 #pragma unroll 1
-    for (int h = 0; h < halves; ++h) {
-        const int id = plan[2 + 2 * h];
+    for (int at = 0; at < blocks; ++at) {
+        const int id = ids[at];
         if (id == last) continue;
         last = id;
         unsigned bad[CF / 2], any = 0;                            // of the lane's eight columns

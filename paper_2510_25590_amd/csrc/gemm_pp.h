@@ -168,14 +168,15 @@ gemm_pp_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
     const int ks_begin = split * steps_per_split;
     int n_steps = K / 64 - ks_begin;
     n_steps = n_steps < steps_per_split ? n_steps : steps_per_split;
-    // low-rank adapters: their K-steps follow the product's own
+    // low-rank adapters: their K-steps follow the product's own; a few steps of its own start before the plan is here
     const int n_own = n_steps;
+    const bool at_once = KIND != EPI_ADAPTERS || n_own >= 3;
     AdapterPlan plan = nullptr;
     if constexpr (KIND == EPI_ADAPTERS) {
         plan = adapter_plan(ep.adapters, m_tile);
-        if (split == splits - 1) n_steps += adapter_steps(plan);
+        if (!at_once && split == splits - 1) n_steps += adapter_steps(plan);
     }
-    const int n_phases = n_steps * (2 / HP);
+    int n_phases = n_steps * (2 / HP);
 
     // Copy sources.  A: a lane copies 16 bytes of one row; LDS rows are 128 bytes, 16-byte chunk c of row r at c ^ ((r >> 1) & 7),
     // the swizzle applied on the global side (rows past M repeat the last row; their results are never stored).
@@ -236,6 +237,7 @@ gemm_pp_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
 #define PP_WAIT() { pp_wait<PENDING>(); __builtin_amdgcn_sched_barrier(0); }
     // the same copies where they may be those of adapters' steps, whose rows come in the order of LDS and whose weights lie where the plan says
     const char* const t_base = KIND == EPI_ADAPTERS ? adapter_terms(ep.adapters, m_tile) + wave * (AC * 1024) : nullptr;
+    AdapterStep theirs_step = {};
 #define PP_COPY_A_END(I0, I1)                                                                               \
     if constexpr (KIND == EPI_ADAPTERS) {                                                                   \
         const int st_ = a_next < n_steps ? a_next : n_steps - 1;                                            \
@@ -248,20 +250,36 @@ gemm_pp_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
 #define PP_COPY_W_END()                                                                                     \
     if constexpr (KIND == EPI_ADAPTERS) {                                                                   \
         static_assert(WC == KB, "a wave copies a phase's k-blocks of one column block");                    \
-        const int ph_ = w_next < n_phases ? w_next : n_phases - 1, half_ = (ph_ - n_own * (2 / HP)) * HP;   \
+        const int ph_ = w_next < n_phases ? w_next : n_phases - 1, at_ = ph_ - n_own * (2 / HP);             \
         const char* const src_ = w_base + static_cast<int64_t>(ph_) * (KB * 1024);                          \
         _Pragma("unroll") for (int c = 0; c < WC; ++c) {                                                    \
-            const char* const theirs_ = adapter_block(ep.adapters, adapter_half(plan, (half_ < 0 ? 0 : half_) + (c >> 1)), c & 1, nb); \
-            pp_copy16(w_voff, half_ >= 0 ? theirs_ : src_ + c * 1024, w_dst + w_slot + c * 1024u);          \
+            const char* const theirs_ = adapter_block(ep.adapters, theirs_step, HP == 2 ? c : 2 * (at_ & 1) + c, nb); \
+            pp_copy16(w_voff, at_ >= 0 ? theirs_ : src_ + c * 1024, w_dst + w_slot + c * 1024u);          \
         }                                                                                                   \
         ++w_next; w_slot = w_slot == (T::W_SLOTS - 1) * T::W_SLOT ? 0 : w_slot + T::W_SLOT;                 \
+        const int then_ = (w_next < n_phases ? w_next : n_phases - 1) / (2 / HP) - n_own;                   \
+        theirs_step = adapter_step(plan, then_ < 0 ? 0 : then_);   /* a phase ahead of its use */           \
     } else PP_COPY_W()
-    PP_COPY_A_END(0, AC) PP_A_DONE() PP_COPY_W_END()
-    if (HP == 2) {
-        PP_COPY_A_END(0, AC) PP_A_DONE() PP_COPY_W_END()
+#define PP_START(COPY_A, COPY_W)                                                                            \
+    {                                                                                                       \
+        COPY_A(0, AC) PP_A_DONE() COPY_W()                                                                  \
+        if (HP == 2) {                                                                                      \
+            COPY_A(0, AC) PP_A_DONE() COPY_W()                                                              \
+        } else {                                                                                            \
+            COPY_A(0, AE) COPY_W()                                                                          \
+            COPY_A(AE, AC) PP_A_DONE() COPY_W()                                                             \
+        }                                                                                                   \
+    }
+    if (at_once) {
+        PP_START(PP_COPY_A, PP_COPY_W)
     } else {
-        PP_COPY_A_END(0, AE) PP_COPY_W_END()
-        PP_COPY_A_END(AE, AC) PP_A_DONE() PP_COPY_W_END()
+        if constexpr (KIND == EPI_ADAPTERS) theirs_step = adapter_step(plan, 0);
+        PP_START(PP_COPY_A_END, PP_COPY_W_END)
+    }
+#undef PP_START
+    if constexpr (KIND == EPI_ADAPTERS) {
+        if (at_once && split == splits - 1) n_steps += adapter_steps(plan);
+        n_phases = n_steps * (2 / HP);
     }
     PP_WAIT()
     pp_barrier();
@@ -319,9 +337,14 @@ gemm_pp_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
         a_rd = a_rd == 2 * T::A_STEP ? 0 : a_rd + T::A_STEP;                                                \
     }
     // (the copies run two steps ahead: up to there they are the product's own)
+    // with adapters always all of a wave's rows (those past M bring anything and are not stored): a second form of each loop costs registers that they need; us, the whole call: 8704 x 9216 x 3072
+    // rank 64 414 -> 407, rank 16 390 -> 385, 4096 x 2048 x 2048 55.7 -> 54.4
     const int n_plain = KIND == EPI_ADAPTERS ? (n_own < 2 ? 0 : n_own - 2) : n_steps;
-    if (live == RF) { PP_LOOP(0, n_plain, RF, PP_COPY_A, PP_COPY_W) } else { PP_LOOP(0, n_plain, live, PP_COPY_A, PP_COPY_W) }
-    if constexpr (KIND == EPI_ADAPTERS) { PP_LOOP(n_plain, n_steps, live, PP_COPY_A_END, PP_COPY_W_END) }
+    if (KIND == EPI_ADAPTERS || live == RF) { PP_LOOP(0, n_plain, RF, PP_COPY_A, PP_COPY_W) } else { PP_LOOP(0, n_plain, live, PP_COPY_A, PP_COPY_W) }
+    if constexpr (KIND == EPI_ADAPTERS) {
+        if (at_once) theirs_step = adapter_step(plan, 0);
+        PP_LOOP(n_plain, n_steps, RF, PP_COPY_A_END, PP_COPY_W_END)
+    }
 #undef PP_LOOP
 #undef PP_PHASE
 #undef PP_COMPUTE
@@ -414,12 +437,12 @@ gemm_kg_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
     const int ks_begin = split * steps_per_split;
     int n_steps = K / 64 - ks_begin;
     n_steps = n_steps < steps_per_split ? n_steps : steps_per_split;
-    // low-rank adapters: their K-steps follow the product's own
+    // low-rank adapters: their K-steps follow the product's own; a few steps of its own start before the plan is here
     const int n_own = n_steps;
+    const bool at_once = KIND != EPI_ADAPTERS || n_own >= NS - 1;
     AdapterPlan plan = nullptr;
     if constexpr (KIND == EPI_ADAPTERS) {
-        plan = adapter_plan(ep.adapters, m_tile);
-        if (split == splits - 1) n_steps += adapter_steps(plan);
+        if (!at_once && split == splits - 1) n_steps += adapter_steps(adapter_plan(ep.adapters, m_tile));
     }
 
     // The copies of a K-step (8 rows of A or one 32-column x 16-k weight block, 1 KiB each) are dealt out to the waves in
@@ -470,11 +493,20 @@ gemm_kg_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
         ++next; buf = buf == (NS - 1) * T::STEP ? 0 : buf + T::STEP;                                        \
     }
     // the same copies where they may be those of adapters' steps, whose rows come in the order of LDS and whose weights lie where the plan says
-    const char* const t_base = KIND == EPI_ADAPTERS ? adapter_terms(ep.adapters, m_tile) : nullptr;
+    const char* t_base = nullptr;
+    AdapterStep theirs_step = {};
+    // (found anew behind the loop: nothing made of them takes scalar registers in it)
+    auto find_adapters = [&]() __attribute__((always_inline)) {
+        int tile = m_tile;
+        asm volatile("" : "+s"(tile));
+        plan = adapter_plan(ep.adapters, tile);
+        t_base = adapter_terms(ep.adapters, tile);
+        const int at = (next < n_steps ? next : n_steps - 1) - n_own;      // of the copy that is next
+        theirs_step = adapter_step(plan, at < 0 ? 0 : at);
+    };
 #define KG_COPY_END()                                                                                       \
     if constexpr (KIND == EPI_ADAPTERS) {                                                                   \
         const int st_ = next < n_steps ? next : n_steps - 1, at_ = st_ - n_own;                             \
-        const AdapterHalf first_ = adapter_half(plan, 2 * (at_ < 0 ? 0 : at_)), second_ = adapter_half(plan, 2 * (at_ < 0 ? 0 : at_) + 1); \
         _Pragma("unroll") for (int i = 0; i < CW; ++i) {                                                    \
             int c_ = wave * CW + i;                                                                         \
             c_ = c_ < T::COPIES ? c_ : T::COPIES - 1;                                                       \
@@ -482,15 +514,26 @@ gemm_kg_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
             const int f_ = rows_ ? 0 : c_ - T::A_COPIES;                                                    \
             int nb_ = (n0 >> 5) + (f_ >> 2);                                                                \
             nb_ = nb_ < n_blocks ? nb_ : n_blocks - 1;                                                      \
-            const char* const block_ = adapter_block(ep.adapters, {f_ & 2 ? second_.id : first_.id, f_ & 2 ? second_.blocks : first_.blocks}, f_ & 1, nb_); \
+            const char* const block_ = adapter_block(ep.adapters, theirs_step, f_ & 3, nb_); \
             const char* const theirs_ = rows_ ? t_base + static_cast<int64_t>(at_) * (T::ROWS * 128) + c_ * 1024 : block_; \
-            pp_copy16(at_ >= 0 && rows_ ? static_cast<unsigned>(lane) * 16u : voff[i], at_ >= 0 ? theirs_ : base[i] + static_cast<uint64_t>(st_) * stride[i], dst[i] + buf); \
+            pp_copy16(at_ >= 0 && rows_ ? static_cast<unsigned>(lane) * 16u : voff[i], at_ >= 0 ? theirs_ : base[i] + static_cast<uint64_t>(st_) * stride[i], lds0 + c_ * 1024u + buf); \
             __builtin_amdgcn_sched_barrier(0);   /* one address at a time in scalar registers */            \
         }                                                                                                   \
         ++next; buf = buf == (NS - 1) * T::STEP ? 0 : buf + T::STEP;                                        \
+        const int then_ = (next < n_steps ? next : n_steps - 1) - n_own;                                    \
+        theirs_step = adapter_step(plan, then_ < 0 ? 0 : then_);   /* a step ahead of its use */            \
     } else KG_COPY()
-#pragma unroll(KIND == EPI_ADAPTERS ? 1 : NS - 1)
-    for (int p = 0; p < NS - 1; ++p) KG_COPY_END()
+    if (at_once) {
+#pragma unroll
+        for (int p = 0; p < NS - 1; ++p) KG_COPY()
+    } else {
+        if constexpr (KIND == EPI_ADAPTERS) find_adapters();
+#pragma unroll 1
+        for (int p = 0; p < NS - 1; ++p) KG_COPY_END()
+    }
+    if constexpr (KIND == EPI_ADAPTERS) {
+        if (at_once && split == splits - 1) n_steps += adapter_steps(adapter_plan(ep.adapters, m_tile));
+    }
     pp_wait<(NS - 2) * CW>();
     pp_barrier();
     if (kg == 1) pp_barrier();     // the second group runs one half phase behind the first
@@ -516,9 +559,13 @@ gemm_kg_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
         pp_barrier();                                                                                       \
     }
     // (the copies run NS - 1 steps ahead: up to there they are the product's own)
+    // with adapters always all of a wave's rows: a second form of each loop costs scalar registers that they need, and 820 x 12288 x 3072 83 -> 73 us without
     const int n_plain = KIND == EPI_ADAPTERS ? (n_own < NS - 1 ? 0 : n_own - (NS - 1)) : n_steps;
-    if (live == RF) { KG_LOOP(0, n_plain, RF, KG_COPY) } else { KG_LOOP(0, n_plain, live, KG_COPY) }
-    if constexpr (KIND == EPI_ADAPTERS) { KG_LOOP(n_plain, n_steps, live, KG_COPY_END) }
+    if (KIND == EPI_ADAPTERS || live == RF) { KG_LOOP(0, n_plain, RF, KG_COPY) } else { KG_LOOP(0, n_plain, live, KG_COPY) }
+    if constexpr (KIND == EPI_ADAPTERS) {
+        find_adapters();
+        KG_LOOP(n_plain, n_steps, RF, KG_COPY_END)
+    }
 #undef KG_LOOP
 #undef KG_COPY_END
 #undef KG_COPY

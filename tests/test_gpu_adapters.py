@@ -114,6 +114,20 @@ def test_every_tile(tile, splits):
     ctx.close()
 
 
+@pytest.mark.parametrize("k", [64, 128, 192, 256])
+@pytest.mark.parametrize("tile", TILES)
+def test_products_shorter_than_their_pipeline(tile, k):
+    """One to four steps of K, so that the copies ahead are the adapters' from the start, then or later; 0 to 15 steps of adapters."""
+    ctx = rg.Context(256, 4, 64, 1024, 64, 64)
+    rg.regione_tune_gemm(ctx, tile, 1)
+    for rank, kind in ((16, "none"), (5, "requests"), (40, "router"), (64, "requests")):
+        o = Operands(ctx, 270, 200, k, rank, 4, 2, kind, tile + k, True)
+        for out in (torch.float32, torch.bfloat16):
+            want = torch.from_numpy(o.reference()[0]).float().to(out)
+            assert torch.equal(o.call(ctx, torch.empty(270, 200, dtype=out, device="cuda")).cpu(), want)
+    ctx.close()
+
+
 def test_without_weights_they_are_one(ctx):
     o = Operands(ctx, 70, 96, 128, 16, 3, 2, "router", 5, True)
     assert np.array_equal(o.call(ctx, torch.empty(70, 96, device="cuda"), weighted=False).cpu().double().numpy(), o.reference(weighted=False)[0])
