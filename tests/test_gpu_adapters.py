@@ -231,6 +231,76 @@ def test_captured_and_replayed_with_other_adapters():
         ctx.close()
 
 
+@pytest.mark.parametrize("m,n", [(5, 72), (300, 520), (300, 267)])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_results_at_any_address(ctx, m, n, out):
+    """... and nothing beside them is written."""
+    o = Operands(ctx, m, n, 192, 12, 3, 2, "router", m + n, True)
+    for shift in (0, 1, 3):
+        room = torch.full((m * n + 16,), 7.0, dtype=out, device="cuda")
+        o.call(ctx, room[shift:shift + m * n].view(m, n))
+        want = torch.from_numpy(o.reference()[0]).float().to(out)
+        assert torch.equal(room[shift:shift + m * n].view(m, n).cpu(), want)
+        assert (room[:shift] == 7).all() and (room[shift + m * n:] == 7).all()
+
+
+@pytest.mark.parametrize("m", [7, 40, 700])
+def test_the_most_adapters(ctx, m):
+    """65536 of them, the first and the last named."""
+    n, k, rank, count = 40, 64, 3, 65536
+    o = Operands(ctx, m, n, k, rank, 3, 2, "router", 11, True)
+    ids = np.array([0, 40000, 65535])
+    packed = torch.zeros(count, o.ap.shape[1], dtype=torch.bfloat16, device="cuda")
+    packed[torch.from_numpy(ids).cuda()] = o.ap
+    o.ap, o.whichd, o.count = packed, up(ids[o.which].astype(np.int32)), count
+    got = o.call(ctx, torch.full((m, n), 7.0, device="cuda"))
+    assert np.array_equal(got.cpu().double().numpy(), o.reference()[0])
+
+
+def test_values_that_are_not_finite_where_tiles_mix(ctx):
+    """Rank 256, every row with one of five adapters; one of them holds an infinity and a NaN in B, one a NaN in A."""
+    m, n, k, rank = 600, 2304, 128, 256
+    o = Operands(ctx, m, n, k, rank, 5, 1, "router", 13, True)
+    b, a = o.b.clone(), o.a.clone()
+    b[3, 5, 200], b[3, 2300, 17], a[1, 255, 127] = float("inf"), float("nan"), float("nan")
+    o.ap = rg.pack_adapters(ctx, a.cuda(), b.cuda())
+    want = torch.from_numpy(o.reference()[0]).float()
+    for out in (torch.float32, torch.bfloat16):
+        got = o.call(ctx, torch.empty(m, n, dtype=out, device="cuda")).cpu()
+        bad = torch.zeros(m, n, dtype=torch.bool)
+        bad[torch.from_numpy(o.which[:, 0] == 1)] = True
+        three = torch.from_numpy(np.flatnonzero(o.which[:, 0] == 3))
+        bad[three, 5] = bad[three, 2300] = True
+        assert torch.equal(torch.isnan(got), bad)
+        assert torch.equal(got[~bad], want.to(out)[~bad])
+
+
+def test_two_graphs_of_one_context():
+    """Both use the context's workspace; replayed in turn, with eager calls between them."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = rg.Context(256, 4, 64, 1024, 64, 64, stream=stream)
+        jobs = []
+        for m, n, k, count in ((700, 640, 512, 4), (300, 1032, 1024, 40)):
+            o = Operands(ctx, m, n, k, 24, count, 2, "router", m, True)
+            y = torch.zeros(m, n, device="cuda")
+            o.call(ctx, y)
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                rg.regione_linear_adapters(ctx, o.xd, o.wp, None, o.ap, o.whichd, o.weightd, o.count, o.sel, o.rank, m, n, k, rg.ACT_NONE, rg.FP32, y)
+            jobs.append((o, y, graph, o.reference()[0]))
+        for i in (0, 1, 1, 0, 1, 0):
+            o, y, graph, want = jobs[i]
+            y.fill_(7.0)
+            graph.replay()
+            assert np.array_equal(y.cpu().double().numpy(), want)
+            other, z, _, expected = jobs[1 - i]
+            assert np.array_equal(other.call(ctx, z.fill_(7.0)).cpu().double().numpy(), expected)
+        del jobs, graph
+        ctx.close()
+
+
 def test_two_contexts_at_once():
     """Each on a stream of its own, with its own workspace."""
     jobs = []
