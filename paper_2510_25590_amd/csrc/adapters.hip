@@ -7,8 +7,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kNoAdapter = 0x7fffffff;
 constexpr int kMostRank = 256, kMostSel = 32, kMostAdapters = 1 << 16;
-constexpr int kLeastChunk = 1024;                        // rows of a pass below which tiles leave their work to the kernel of 16 rows
-constexpr size_t kTermBytes = size_t{32} << 20;          // of the inner products of the rows that go through at a time
+constexpr size_t kTermBytes = size_t{64} << 20;          // of the inner products of the rows that go through at a time
 
 // A packed adapter: behind A and B a bit per column of B that holds a value that is not finite (zero in B), 32 to a word, a word that is not zero if there is one, and zeros up to 16 bytes.
 // A in fragments of 16 ranks x 32 inputs, 64 lanes x 8 values, lane l holding A[16 * (block) + l % 16][32 * step + 8 * (l / 16) .. +8]; behind it B as regione_pack_weight
@@ -419,13 +418,15 @@ extern "C" int regione_linear_adapters(regione_ctx* ctx, const void* x, const vo
     // the most that a tile can name: every row another adapter
     const int64_t named = static_cast<int64_t>(tiles.rows) * n_sel < n_adapters ? static_cast<int64_t>(tiles.rows) * n_sel : n_adapters, tile_steps = (named * terms * blocks + 3) / 4;
     const int64_t tile_bytes = tile_steps * tiles.rows * 128, plan_words = 4 + 12 * tile_steps, plan_bytes = plan_words * 4, fits = static_cast<int64_t>(room) / (tile_bytes + plan_bytes), m_tiles = (m + tiles.rows - 1) / tiles.rows;
+    // More than fits goes through in passes of whole tiles; a tile that does not fit leaves the call to the kernel of 16 rows, which reads what its rows name and no more.  us, passes / that kernel, 500 adapters,
+    // 4096 x 2048: 8192 rows, rank 16, a request every 64 rows 180 / 943, every row any adapter 911 / 1095; 2048 rows, rank 64 83 / 340 and 648 / 598 (with 32 MB in place of 64: 260, 1473, 113 and 909)
     int64_t chunk = m;
     if (tiles.tile && fits < m_tiles) {
-        if (fits * tiles.rows >= kLeastChunk) {
+        if (fits > 0) {
             chunk = fits * tiles.rows;
             tiles.splits = 1;
         } else {
-            tiles = {0, 1, 16};                                   // the kernel of 16 rows reads what its rows name and no more
+            tiles = {0, 1, 16};
         }
     }
     const size_t row_bytes = static_cast<size_t>(n_sel) * cols * 2;

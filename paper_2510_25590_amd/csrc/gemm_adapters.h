@@ -78,7 +78,7 @@ template <int CF> __device__ __forceinline__ void adapter_weights(const AdapterR
         w[2 * b + 1] = *reinterpret_cast<const bf16x8*>(from + at + 32);
     }
 }
-// rows of terms, all of them within 32 MB; what lies outside, such as no place at all, is zero by the resource's size
+// rows of terms, all of them within 64 MB; what lies outside, such as no place at all, is zero by the resource's size
 __device__ __forceinline__ auto adapter_terms_rsrc(const AdapterRows& ad, int M) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(ad.t), 0, M * ad.sel * ad.cols * 2, 0x00027000); }
 constexpr unsigned kNoTerms = 0xfffffff0u;
 

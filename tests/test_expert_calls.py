@@ -146,9 +146,9 @@ def test_every_adapter_product_covers_its_result(run):
             assert dx == -(-m // tile[0]) * -(-tile[0] // rows) and dy >= 1
     assert {s[0] for s in seen} == {"small", "pp", "kg"}
     many = run([BF, adapters(m=2000, n=64, k=64, rank=256, sel=32, out=1)])[1]
-    assert len(many[1]) == 2 * 3                                         # 672 rows at a time
-    # where every row of a tile may name another adapter: passes of as many tiles as the workspace holds, or, below 1024 rows, the kernel of 16 rows
-    passes, single = run([BF, adapters(m=4200, n=2304, k=128, rank=8, count=600), adapters(m=4200, n=2304, k=128, rank=8, count=5000, sel=4)])[1:]
+    assert len(many[1]) == 2 * 2                                         # 1360 rows at a time
+    # where every row of a tile may name another adapter: passes of as many tiles as the workspace holds, or the kernel of 16 rows where a tile does not fit
+    passes, single = run([BF, adapters(m=20000, n=2304, k=128, rank=8, count=600), adapters(m=4200, n=2304, k=128, rank=8, count=20000, sel=32)])[1:]
     assert len(passes[1]) > 2 and len(passes[1]) % 2 == 0 and all(re.search("gemm_(pp|kg)", kernel) for _, _, kernel in passes[1][1::2])
     assert len(single[1]) == 2 and "gemm_small" in single[1][1][2]
 

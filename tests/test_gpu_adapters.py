@@ -161,17 +161,17 @@ def test_rows_without_adapters_are_the_plain_product(ctx, m, n):
 
 
 def test_more_inner_products_than_are_kept_at_a_time(ctx):
-    """32 adapters of rank 256 per row, float32: 672 rows at a time."""
-    o = Operands(ctx, 1100, 64, 64, 256, 40, 32, "router", 7, True)
+    """32 adapters of rank 256 per row, float32: 1360 rows at a time."""
+    o = Operands(ctx, 1500, 64, 64, 256, 40, 32, "router", 7, True)
     o.which[:, 8:] = -1                                                  # (the reference's time)
     o.which[:, 31] = 39
     o.whichd = up(o.which)
-    assert np.array_equal(o.call(ctx, torch.empty(1100, 64, device="cuda")).cpu().double().numpy(), o.reference()[0])
+    assert np.array_equal(o.call(ctx, torch.empty(1500, 64, device="cuda")).cpu().double().numpy(), o.reference()[0])
 
 
-@pytest.mark.parametrize("count,sel", [(600, 1), (5000, 4)])
+@pytest.mark.parametrize("count,sel", [(600, 1), (5000, 4), (20000, 16)])
 def test_many_adapters_in_a_tile(ctx, count, sel):
-    """Tiles that may name more adapters than the workspace has room for: passes over the rows; and the kernel of 16 rows."""
+    """Tiles that may name more adapters than the workspace has room for: passes over the rows, of few tiles, and the kernel of 16 rows."""
     m, n, k = 4200, 2304, 128
     o = Operands(ctx, m, n, k, 8, 8, sel, "router", 8, True)
     rng = np.random.default_rng(3)
