@@ -198,15 +198,9 @@ _COPY = "global_load_lds_dwordx4"
 _WIDE_STORE = re.compile(r"^(buffer|global)_store_dwordx[34]\b")
 
 
-def _waits_for_all(instrs) -> bool:
-    return any(a and i.startswith("s_waitcnt") and (m := _VMCNT.search(i)) is not None and int(m.group(1)) == 0 for i, a in instrs)
-
-
 def check_copies(name: str, lines) -> list[str]:
     """The two-group kernels count their global-to-LDS copies by hand: inside a K loop (every basic block that runs MFMAs or
-    such copies and is reached again from itself) no other vector-memory instruction may stand, or the counts are off.
-    A loop of MFMAs that issues no copy and that none can be in flight in (a wait for all of them lies on every way from a
-    copy to it) is no K loop: the low-rank adapters behind the product load their operands as the compiler likes."""
+    such copies and is reached again from itself) no other vector-memory instruction may stand, or the counts are off."""
     blocks = _blocks(lines)
     short = name[:70]
     errors = []
@@ -219,24 +213,8 @@ def check_copies(name: str, lines) -> list[str]:
                 seen.add(b)
                 work += blocks[b][2]
         reach.append(seen)
-    copies = [k for k, b in enumerate(blocks) if any(i.startswith(_COPY) for i, _ in b[1])]
-    # blocks that a copy can be in flight in: reached from behind a copy without a wait for all
-    flying: set[int] = set()
-    for k in copies:
-        last = max(n for n, (i, _) in enumerate(blocks[k][1]) if i.startswith(_COPY))
-        if _waits_for_all(blocks[k][1][last:]):
-            continue
-        work = list(blocks[k][2])
-        while work:
-            b = work.pop()
-            if b not in flying:
-                flying.add(b)
-                if not _waits_for_all(blocks[b][1]):
-                    work += blocks[b][2]
     for k, b in enumerate(blocks):
         if k not in reach[k] or not any(i.startswith(_COPY) or i.startswith("v_mfma") for i, _ in b[1]):
-            continue
-        if k not in flying and not any(c in reach[k] and k in reach[c] for c in copies):
             continue
         for instr, in_asm in b[1]:
             op = instr.split()[0]
