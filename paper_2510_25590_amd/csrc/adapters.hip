@@ -138,13 +138,13 @@ adapters_down_rows_kernel(DownCall d) {
 }
 
 // For tiles (their layout and plan: gemm_adapters.h): a workgroup owns 16 * RB rows and goes through the blocks of 16 ranks of their adapters, NB at a time; those of the tile that none of the
-// rows names are zeros there.  Workgroups of the same rows (blockIdx.y) take turns.  WAVES waves split K and meet in LDS, where the sums are formed in wave order.
+// rows names are zeros there.  Without a plan (many rows for the kernel of 16): the layout above, every workgroup's rows by themselves.  Workgroups of the same rows (blockIdx.y) take turns.  WAVES waves split K and meet in LDS, where the sums are formed in wave order.
 // The rows come in whole lines, 8 x 128 bytes to a load, and change to fragments in a part of LDS that is the wave's own.  What bounds it is the way from L2 into a CU, 20 bytes a cycle: all of A
 // for every workgroup beside its rows, so that 32 rows to a workgroup pay where there are workgroups enough.  8704 rows, K 3072, rank 64: 24 us (33 with x from HBM), 6 of them the launch and the list of the
 // adapters; with A from L1 20, with x from L1 too 18.  As fragments from memory, 64 bytes of 16 rows to a load, x took half as long again.
 // Steps past a wave's own are multiplied with zeros: a branch around the products lets the compiler move the loads into it, behind all that should hide them.
 struct DownTiles { int rows, plan_pitch; int64_t tile_elems; int32_t* plan; int64_t bad; };      // rows of a tile; elements of an adapter ahead of its bits
-template <int RB, int NB, int WAVES>
+template <bool PLANNED, int RB, int NB, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64)
 adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
     constexpr int T = WAVES * 64, ROWS = 16 * RB, AHEAD = 2;
@@ -159,9 +159,9 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
     f32x4 (*const sums)[NB][64] = reinterpret_cast<f32x4 (*)[NB][64]>(lds);
     const int lane = threadIdx.x & 63, l16 = lane & 15, kc = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int pieces = (tiles.rows + ROWS - 1) / ROWS, tile = blockIdx.x / pieces, row0 = (blockIdx.x - tile * pieces) * ROWS;
-    const int t0 = tile * tiles.rows, tile_rows = d.m - t0 < tiles.rows ? d.m - t0 : tiles.rows, m0 = t0 + row0;
-    const int rows = tile_rows - row0 < ROWS ? tile_rows - row0 : ROWS, place_rows = tiles.rows - row0 < ROWS ? tiles.rows - row0 : ROWS;
+    const int pieces = PLANNED ? (tiles.rows + ROWS - 1) / ROWS : 1, tile = blockIdx.x / pieces, row0 = (blockIdx.x - tile * pieces) * ROWS;
+    const int most_rows = PLANNED ? tiles.rows : ROWS, t0 = tile * most_rows, tile_rows = d.m - t0 < most_rows ? d.m - t0 : most_rows, m0 = t0 + row0;
+    const int rows = tile_rows - row0 < ROWS ? tile_rows - row0 : ROWS, place_rows = most_rows - row0 < ROWS ? most_rows - row0 : ROWS;
     if (rows <= 0) return;                                        // (the last tile's end)
     const int steps = d.k >> 6, share = (steps + WAVES - 1) / WAVES, s0 = wave * share;    // of 64 inputs
     const int own = s0 + share < steps ? share : (steps > s0 ? steps - s0 : 0);
@@ -199,12 +199,12 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
     }
     __syncthreads();
 
-    unsigned char* const t = reinterpret_cast<unsigned char*>(d.t + tile * tiles.tile_elems);
+    unsigned char* const t = reinterpret_cast<unsigned char*>(d.t + (PLANNED ? tile * tiles.tile_elems : static_cast<int64_t>(m0) * d.sel * d.cols));
     auto place = [&](int row, int of, int c) __attribute__((always_inline)) {       // column c of a block of 16 terms, in the order of LDS
         return t + (static_cast<int64_t>(of >> 2) * tiles.rows + row) * 128 + ((((of & 3) * 2 + (c >> 3)) ^ ((row >> 1) & 7)) << 4) + (c & 7) * 2;
     };
     const int per = d.terms * d.blocks;                           // blocks of 16 terms of an adapter
-    const bool lead = row0 == 0 && blockIdx.y == 0;
+    const bool lead = PLANNED && row0 == 0 && blockIdx.y == 0;
     int32_t* const plan = tiles.plan + static_cast<int64_t>(tile) * tiles.plan_pitch;
     int64_t* const offsets = reinterpret_cast<int64_t*>(plan + 4);
     const int ids_at = 4 + (tiles.plan_pitch - 4) / 3 * 2;
@@ -244,7 +244,7 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
             }
             if (threadIdx.x == 0) bad |= *reinterpret_cast<const uint32_t*>(d.packed + static_cast<int64_t>(a) * d.stride + tiles.bad);
         }
-        if (!in_rows && pos % gridDim.y == blockIdx.y) zeros(pos * per, per);
+        if (PLANNED && !in_rows && pos % gridDim.y == blockIdx.y) zeros(pos * per, per);
     };
     bool first_batch = true;
     for (unsigned batch = 0; a != kNoAdapter; ++batch) {
@@ -315,16 +315,20 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
 #pragma unroll
                     for (int v = 1; v < WAVES; ++v) sum += sums[v][q][lane];
                     const int row = 16 * i + l16, first = unit_pos[q] * per;
-                    bool its = false;
+                    int at = -1;                                  // the row's first place of the adapter, and its weights
                     float w = 0.f;
                     if (row < rows)
                         for (int s = d.sel - 1; s >= 0; --s)
-                            if (ids[row * d.sel + s] == unit_a[q]) { its = true; w += weights[row * d.sel + s]; }
-                    if (row < place_rows) put_terms([&](int c) { return place(row0 + row, first + (c >> 4), c & 15); }, kc, unit_block[q], d.blocks, d.terms, 0, w, sum, its);
+                            if (ids[row * d.sel + s] == unit_a[q]) { at = s; w += weights[row * d.sel + s]; }
+                    if (!PLANNED) {
+                        bf16_t* const to = reinterpret_cast<bf16_t*>(t) + (row * d.sel + at) * d.cols;
+                        if (at >= 0) put_terms([&](int c) { return to + c; }, kc, unit_block[q], d.blocks, d.terms, d.cols, w, sum);
+                    } else if (row < place_rows) put_terms([&](int c) { return place(row0 + row, first + (c >> 4), c & 15); }, kc, unit_block[q], d.blocks, d.terms, 0, w, sum, at >= 0);
                 }
             __syncthreads();
         }
     }
+    if (!PLANNED) return;
     const int all = (pos + 1) * per, filled = (all + 3) & ~3;     // whole steps
     if (filled > all && blockIdx.y == 0) zeros(all, filled - all);
     if (lead && threadIdx.x == 0) {
@@ -335,26 +339,37 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
     }
 }
 
-int down_rows(regione_ctx* ctx, const DownCall& d) {
-    hipLaunchKernelGGL(adapters_down_rows_kernel, dim3(static_cast<unsigned>((d.m + 15) / 16), static_cast<unsigned>((d.m < 16 ? d.m : 16) * d.sel * d.blocks)), dim3(kDownWaves * 64), 0, ctx->stream, d);
-    RG_LAUNCH_CHECK();
-    return REGIONE_OK;
-}
-
-template <int RB, int NB, int WAVES>
-void launch_down_tiles(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
-    const int pieces = (d.m + tiles.rows - 1) / tiles.rows * ((tiles.rows + 16 * RB - 1) / (16 * RB));
+template <bool PLANNED, int RB, int NB, int WAVES>
+void launch_down(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
+    const int rows = PLANNED ? tiles.rows : 16 * RB, pieces = (d.m + rows - 1) / rows * ((rows + 16 * RB - 1) / (16 * RB));
     const int64_t most = static_cast<int64_t>(16 * RB) * d.sel < d.count ? static_cast<int64_t>(16 * RB) * d.sel : d.count, batches = (most * d.blocks + NB - 1) / NB;
     const int64_t room = pieces < 512 ? 512 / pieces : 1;
-    hipLaunchKernelGGL((adapters_down_tiles_kernel<RB, NB, WAVES>), dim3(pieces, static_cast<unsigned>(batches < room ? batches : room)), dim3(WAVES * 64), 0, ctx->stream, d, tiles);
+    hipLaunchKernelGGL((adapters_down_tiles_kernel<PLANNED, RB, NB, WAVES>), dim3(pieces, static_cast<unsigned>(batches < room ? batches : room)), dim3(WAVES * 64), 0, ctx->stream, d, tiles);
 }
-int down_tiles(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
+template <bool PLANNED> void launch_down(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
     // us, K 3072, a block of ranks to a workgroup / four / four of 32 rows: 820 rows, rank 16 6.5 / 8.2 / 10.1, rank 64 10.9 / 10.3 / 12.3; 2048 rows, rank 16 6.8 / 8.2 / 9.8, rank 64
     // 12.6 / 10.5 / 12.1; 4096 rows, rank 16 10.8 / 9.1 / 10.4, rank 64 18.1 / 12.1 / 12.7; 6144 rows, rank 64 24.9 / 16.8 / 14.8; 8704 rows, rank 64 46 / 24.7 / 24.4; 16384 rows 68 / 43 / 34
     const int64_t pieces = (d.m + 15) / 16, units = pieces * d.blocks * (d.sel < d.count ? d.sel : d.count);
-    if (units <= 192) launch_down_tiles<1, 1, 8>(ctx, d, tiles);
-    else if (pieces <= 256) launch_down_tiles<1, 4, 4>(ctx, d, tiles);
-    else launch_down_tiles<2, 4, 4>(ctx, d, tiles);
+    if (units <= 192) launch_down<PLANNED, 1, 1, 8>(ctx, d, tiles);
+    else if (pieces <= 256) launch_down<PLANNED, 1, 4, 4>(ctx, d, tiles);
+    else launch_down<PLANNED, 2, 4, 4>(ctx, d, tiles);
+}
+int down_tiles(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
+    launch_down<true>(ctx, d, tiles);
+    RG_LAUNCH_CHECK();
+    return REGIONE_OK;
+}
+// Places with their blocks of ranks, of all the 16 rows, up to which each has a workgroup: it fills the chip where rows name many adapters, and loads what the earlier places of its 16 rows load as well.  us, the
+// whole call, a workgroup to a place / the kernel above: 40 rows, two of 64 adapters of rank 16 each, 3072 x 3072 (96 places) 20.5 / 29.3; 128 rows, two of eight, 2048 x 2048 (256) 15.7 / 17.9; 64 rows, one of
+// four of rank 64, 3072 x 3072 (256) 17.8 / 17.4; 48 rows, two of six of rank 64 (384) 22.1 / 21.8; 820 rows, rank 16, 64 x 3072 (832) 20.5 / 14.3; 8704 rows, rank 64, 64 x 3072 (34816) 342 / 51
+constexpr int64_t kDownPlaces = 512;
+int down_rows(regione_ctx* ctx, const DownCall& d) {
+    const int64_t tiles = (d.m + 15) / 16, places = static_cast<int64_t>(d.m < 16 ? d.m : 16) * d.sel * d.blocks;
+    if (tiles * places <= kDownPlaces) {
+        hipLaunchKernelGGL(adapters_down_rows_kernel, dim3(static_cast<unsigned>(tiles), static_cast<unsigned>(places)), dim3(kDownWaves * 64), 0, ctx->stream, d);
+    } else {
+        launch_down<false>(ctx, d, DownTiles{});
+    }
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }

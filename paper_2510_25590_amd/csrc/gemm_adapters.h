@@ -85,15 +85,20 @@ __device__ __forceinline__ auto adapter_terms_rsrc(const AdapterRows& ad, int M)
 constexpr unsigned kNoTerms = 0xfffffff0u;
 
 // For the 16 rows that several waves share (gemm_small.h): t [rows, sel, cols], each adapter's terms at the first of the row's places that name it.  A unit of work is a step of 32 terms of an
-// adapter that no earlier row or place of the tile names; wave `turn` of `turns` takes every unit that is its turn.  The first units' operands are requested ahead of the product (fetch, then
-// add behind it).
+// adapter that no earlier row or place of the tile names; wave `turn` of `turns` takes every unit that is its turn.  The tile's list of adapters is asked for ahead of the product's first loads
+// (ask) and looked at behind them, when it has come and they have not; the first units' operands fly under the product (fetch, then add behind it).  Lists of up to 64 places stay in a register.
 template <int CF> struct AdapterUnits {
     static constexpr int AHEAD = 2;
     bf16x8 wf[AHEAD][CF];
     u32x4 tf[AHEAD];
     unsigned bad[AHEAD][CF / 2];                                  // of the lane's columns, where its row names the adapter
     bool there[AHEAD];
-    int next;
+    int next, ids;
+
+    __device__ __forceinline__ void ask(const AdapterRows& ad, int M, int m0) {
+        const int lane = threadIdx.x & 63, entries = (M - m0 < 16 ? M - m0 : 16) * ad.sel;
+        ids = ad.which[static_cast<int64_t>(m0) * ad.sel + (lane < entries ? lane : 0)];
+    }
 
     __device__ __forceinline__ void load(const AdapterRows& ad, int M, int N, int m0, int n0, int q, int unit, int units, int turns) {
         const int lane = threadIdx.x & 63, l16 = lane & 15, kc = lane >> 4, steps = ad.cols >> 5;
@@ -102,14 +107,21 @@ template <int CF> struct AdapterUnits {
         const int32_t* const which = ad.which + static_cast<int64_t>(m0) * ad.sel;
         if (unit >= units) return;
         const int entry = unit / steps, st = unit - entry * steps;
-        const int a = __builtin_amdgcn_readfirstlane(which[entry]);
+        const bool held = rows * ad.sel <= 64;
+        const int a = held ? __builtin_amdgcn_readlane(ids, entry) : __builtin_amdgcn_readfirstlane(which[entry]);
         if (a < 0 || a >= ad.count) return;
-        for (int i = 0; i < entry; i += 64)                       // named before?
-            if (__ballot(i + lane < entry && which[i + lane < entry ? i + lane : 0] == a)) return;
+        if (held) {
+            if (__ballot(lane < entry && ids == a)) return;       // named before
+        } else {
+            for (int i = 0; i < entry; i += 64)
+                if (__ballot(i + lane < entry && which[i + lane < entry ? i + lane : 0] == a)) return;
+        }
         unsigned at = kNoTerms;
-        if (l16 < rows)
-            for (int s = ad.sel - 1; s >= 0; --s)
-                if (which[l16 * ad.sel + s] == a) at = (static_cast<unsigned>(m0 + l16) * ad.sel + s) * (ad.cols * 2u) + 64u * st + 16u * kc;
+        for (int s = ad.sel - 1; s >= 0; --s) {
+            const int of = l16 * ad.sel + s;
+            const int id = held ? __builtin_amdgcn_ds_bpermute(of * 4, ids) : l16 < rows ? which[of] : -1;
+            if (l16 < rows && id == a) at = (static_cast<unsigned>(m0 + l16) * ad.sel + s) * (ad.cols * 2u) + 64u * st + 16u * kc;
+        }
         there[q] = true;
         tf[q] = __builtin_amdgcn_raw_buffer_load_b128(adapter_terms_rsrc(ad, M), at, 0, 0);
         adapter_weights<CF>(ad, a, N, n0, 2 * st % ad.blocks, wf[q]);

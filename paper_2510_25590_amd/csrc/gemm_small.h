@@ -69,7 +69,7 @@ __device__ __forceinline__ void gemm_small_tile(unsigned char* lds, int tile_y, 
     }
 
     typename std::conditional<KIND == EPI_ADAPTERS, AdapterUnits<CF>, char>::type units;
-    if constexpr (KIND == EPI_ADAPTERS) units.fetch(ep.adapters, M, N, m0, n0, wave, kSmallWaves);
+    if constexpr (KIND == EPI_ADAPTERS) units.ask(ep.adapters, M, m0);
     f32x4 acc[CF];
 #pragma unroll
     for (int j = 0; j < CF; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -104,9 +104,14 @@ __device__ __forceinline__ void gemm_small_tile(unsigned char* lds, int tile_y, 
         }
         __syncthreads();
     }
+    if constexpr (KIND == EPI_ADAPTERS) {
+        load_w(s0);
+        load_a(s0);
+        units.fetch(ep.adapters, M, N, m0, n0, wave, kSmallWaves);
+    }
     for (int base = s0; base < s1; base += CHUNK) {
-        if (LN == LN_NONE || base > s0) load_w(base);
-        load_a(base);
+        if (base > s0 || (LN == LN_NONE && KIND != EPI_ADAPTERS)) load_w(base);
+        if (base > s0 || KIND != EPI_ADAPTERS) load_a(base);
 #pragma unroll
         for (int i = 0; i < CHUNK; ++i)
             if (base + i < s1) {

@@ -137,12 +137,14 @@ def test_every_adapter_product_covers_its_result(run):
         seen.add((kind,) + tuple(args))
         assert lds <= 163840
         if kind == "small":
-            assert "adapters_down_rows" in down and dx == -(-m // 16) and dy >= 1
+            of_pieces = re.search(r"adapters_down_tiles_kernel<false, (\d+), ", down)
+            assert of_pieces or "adapters_down_rows" in down
+            assert dx == -(-m // (16 * int(of_pieces.group(1)) if of_pieces else 16)) and dy >= 1
             assert x == -(-n // (16 * args[0])) and y == -(-m // 16)
         else:
             tile = (32 * args[0], 64 * args[1]) if kind == "pp" else (16 * args[0] * args[2], 16 * args[1] * (4 // args[2]))
             assert x >= -(-m // tile[0]) * -(-n // tile[1]) and y == 1
-            rows = 16 * int(re.search(r"adapters_down_tiles_kernel<(\d+), ", down).group(1))
+            rows = 16 * int(re.search(r"adapters_down_tiles_kernel<true, (\d+), ", down).group(1))
             assert dx == -(-m // tile[0]) * -(-tile[0] // rows) and dy >= 1
     assert {s[0] for s in seen} == {"small", "pp", "kg"}
     many = run([BF, adapters(m=2000, n=64, k=64, rank=256, sel=32, out=1)])[1]

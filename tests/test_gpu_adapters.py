@@ -169,6 +169,17 @@ def test_more_inner_products_than_are_kept_at_a_time(ctx):
     assert np.array_equal(o.call(ctx, torch.empty(1500, 64, device="cuda")).cpu().double().numpy(), o.reference()[0])
 
 
+@pytest.mark.parametrize("kind", ["requests", "router", "anything"])
+@pytest.mark.parametrize("m,n,k,rank,count,sel", [(3000, 64, 192, 40, 5, 2), (600, 7, 128, 256, 3, 1), (8704, 33, 64, 16, 4, 1), (530, 64, 64, 9, 100, 5), (4097, 1, 320, 33, 7, 3)])
+def test_narrow_results_of_many_rows(ctx, m, n, k, rank, count, sel, kind):
+    """... which the kernel of 16 rows takes; whole numbers, and nothing behind the last row."""
+    o = Operands(ctx, m, n, k, rank, count, sel, kind, m + n, True)
+    for out in (torch.float32, torch.bfloat16):
+        room = torch.full((m + 1, n), 7.0, dtype=out, device="cuda")
+        o.call(ctx, room[:m])
+        assert torch.equal(room[:m].cpu(), torch.from_numpy(o.reference()[0]).float().to(out)) and (room[m] == 7).all()
+
+
 @pytest.mark.parametrize("count,sel", [(600, 1), (5000, 4), (20000, 16)])
 def test_many_adapters_in_a_tile(ctx, count, sel):
     """Tiles that may name more adapters than the workspace has room for: passes over the rows, of few tiles, and the kernel of 16 rows."""
