@@ -182,6 +182,8 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
 #pragma unroll
         for (int i = 0; i < 2 * RB; ++i) xr[c][i] = *reinterpret_cast<const u32x4*>(xp[i] + step_of(c) * 64);
 
+    const bool lead = PLANNED && row0 == 0 && blockIdx.y == 0;     // writes the tile's plan
+    uint32_t bad = 0;                                             // (looked at here, side by side; one after the other as the list goes, 1711 rows with 23 adapters, K 320, 14.5 -> 16.1 us)
     const int words = (d.count + 31) / 32;
     for (int i = threadIdx.x; i < words; i += T) named[0][i] = named[1][i] = 0u;
     __syncthreads();
@@ -191,6 +193,7 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
         if (counts) {
             atomicOr(&named[0][id >> 5], 1u << (id & 31));
             if (here) atomicOr(&named[1][id >> 5], 1u << (id & 31));
+            if (lead) bad |= *reinterpret_cast<const uint32_t*>(d.packed + static_cast<int64_t>(id) * d.stride + tiles.bad);
         }
         if (here) {
             ids[at] = counts ? id : kNoAdapter;
@@ -204,7 +207,6 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
         return t + (static_cast<int64_t>(of >> 2) * tiles.rows + row) * 128 + ((((of & 3) * 2 + (c >> 3)) ^ ((row >> 1) & 7)) << 4) + (c & 7) * 2;
     };
     const int per = d.terms * d.blocks;                           // blocks of 16 terms of an adapter
-    const bool lead = PLANNED && row0 == 0 && blockIdx.y == 0;
     int32_t* const plan = tiles.plan + static_cast<int64_t>(tile) * tiles.plan_pitch;
     int64_t* const offsets = reinterpret_cast<int64_t*>(plan + 4);
     const int ids_at = 4 + (tiles.plan_pitch - 4) / 3 * 2;
@@ -215,34 +217,43 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
 
     int a = -1, last = 0, pos = -1, block = d.blocks;
     bool in_rows = false;
-    uint32_t bad = 0;
-    auto next_adapter = [&]() __attribute__((always_inline)) {    // the tile's next one, in order
+    const uint32_t tile_word = lane < words ? named[0][lane] : 0u, rows_word = lane < words ? named[1][lane] : 0u;
+    auto next_adapter = [&]() __attribute__((always_inline)) {    // the tile's next one, in order (its words from LDS one by one: 1711 rows with 23 adapters 12.5 -> 14.5 us)
         int w = (a + 1) >> 5;
         uint32_t mask = ~0u << ((a + 1) & 31);
         a = kNoAdapter;
-        while (w < words) {
-            const int at = w + lane;
-            uint32_t v = at < words ? named[0][at] : 0u;
-            if (lane == 0) v &= mask;
-            mask = ~0u;
+        if (words <= 64) {                                        // all words in the wave's registers
+            const uint32_t v = lane < w ? 0u : lane == w ? tile_word & mask : tile_word;
             const uint64_t some = __ballot(v != 0u);
             if (some) {
                 const int first = __builtin_ctzll(some);
-                a = (w + first) * 32 + __builtin_ctz(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(v), first)));
-                break;
+                a = first * 32 + __builtin_ctz(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(v), first)));
+                in_rows = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(rows_word), first)) >> (a & 31) & 1u;
             }
-            w += 64;
+        } else {
+            while (w < words) {
+                const int at = w + lane;
+                uint32_t v = at < words ? named[0][at] : 0u;
+                if (lane == 0) v &= mask;
+                mask = ~0u;
+                const uint64_t some = __ballot(v != 0u);
+                if (some) {
+                    const int first = __builtin_ctzll(some);
+                    a = (w + first) * 32 + __builtin_ctz(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(v), first)));
+                    in_rows = named[1][a >> 5] >> (a & 31) & 1u;
+                    break;
+                }
+                w += 64;
+            }
         }
         if (a == kNoAdapter) return;
         ++pos;
         last = a;
-        in_rows = named[1][a >> 5] >> (a & 31) & 1u;
         if (lead) {
             for (int i = threadIdx.x; i < per; i += T) {
                 offsets[pos * per + i] = (a * d.stride + (i % d.blocks) * 512) * 2;
                 plan[ids_at + pos * per + i] = a;
             }
-            if (threadIdx.x == 0) bad |= *reinterpret_cast<const uint32_t*>(d.packed + static_cast<int64_t>(a) * d.stride + tiles.bad);
         }
         if (PLANNED && !in_rows && pos % gridDim.y == blockIdx.y) zeros(pos * per, per);
     };
@@ -331,14 +342,20 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
     if (!PLANNED) return;
     const int all = (pos + 1) * per, filled = (all + 3) & ~3;     // whole steps
     if (filled > all && blockIdx.y == 0) zeros(all, filled - all);
-    if (lead && threadIdx.x == 0) {
+    if (!lead) return;
+    const int any = __syncthreads_or(bad != 0u);
+    if (threadIdx.x == 0) {
         plan[0] = filled / 4;
-        plan[1] = static_cast<int32_t>(bad);
+        plan[1] = any;
         plan[2] = ids_at;
         for (int i = all; i < filled; ++i) { offsets[i] = last * d.stride * 2; plan[ids_at + i] = last; }
     }
 }
 
+// Places with their blocks of ranks, of all the 16 rows, up to which each has a workgroup: it fills the chip where rows name many adapters, and loads what the earlier places of its 16 rows load as well.  us, the
+// whole call, a workgroup to a place (adapters_down_rows_kernel) / the other kernel: 40 rows, two of 64 adapters of rank 16 each, 3072 x 3072 (96 places) 20.5 / 29.3; 128 rows, two of eight, 2048 x 2048 (256) 15.7 / 17.9; 64 rows, one of
+// four of rank 64, 3072 x 3072 (256) 17.8 / 17.4; 48 rows, two of six of rank 64 (384) 22.1 / 21.8; 820 rows, rank 16, 64 x 3072 (832) 20.5 / 14.3; 8704 rows, rank 64, 64 x 3072 (34816) 342 / 51
+constexpr int64_t kDownPlaces = 512;
 template <bool PLANNED, int RB, int NB, int WAVES>
 void launch_down(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
     const int rows = PLANNED ? tiles.rows : 16 * RB, pieces = (d.m + rows - 1) / rows * ((rows + 16 * RB - 1) / (16 * RB));
@@ -349,8 +366,9 @@ void launch_down(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
 template <bool PLANNED> void launch_down(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
     // us, K 3072, a block of ranks to a workgroup / four / four of 32 rows: 820 rows, rank 16 6.5 / 8.2 / 10.1, rank 64 10.9 / 10.3 / 12.3; 2048 rows, rank 16 6.8 / 8.2 / 9.8, rank 64
     // 12.6 / 10.5 / 12.1; 4096 rows, rank 16 10.8 / 9.1 / 10.4, rank 64 18.1 / 12.1 / 12.7; 6144 rows, rank 64 24.9 / 16.8 / 14.8; 8704 rows, rank 64 46 / 24.7 / 24.4; 16384 rows 68 / 43 / 34
-    const int64_t pieces = (d.m + 15) / 16, units = pieces * d.blocks * (d.sel < d.count ? d.sel : d.count);
-    if (units <= 192) launch_down<PLANNED, 1, 1, 8>(ctx, d, tiles);
+    // A block of ranks to a workgroup only where all that 16 rows may name have one: 1711 rows, any of 23 adapters of rank 9, K 320, four workgroups to 16 rows, 20.7 us against 16.1
+    const int64_t pieces = (d.m + 15) / 16, most = static_cast<int64_t>(16) * d.sel < d.count ? static_cast<int64_t>(16) * d.sel : d.count;
+    if (pieces * most * d.blocks <= kDownPlaces) launch_down<PLANNED, 1, 1, 8>(ctx, d, tiles);
     else if (pieces <= 256) launch_down<PLANNED, 1, 4, 4>(ctx, d, tiles);
     else launch_down<PLANNED, 2, 4, 4>(ctx, d, tiles);
 }
@@ -359,10 +377,6 @@ int down_tiles(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
     RG_LAUNCH_CHECK();
     return REGIONE_OK;
 }
-// Places with their blocks of ranks, of all the 16 rows, up to which each has a workgroup: it fills the chip where rows name many adapters, and loads what the earlier places of its 16 rows load as well.  us, the
-// whole call, a workgroup to a place / the kernel above: 40 rows, two of 64 adapters of rank 16 each, 3072 x 3072 (96 places) 20.5 / 29.3; 128 rows, two of eight, 2048 x 2048 (256) 15.7 / 17.9; 64 rows, one of
-// four of rank 64, 3072 x 3072 (256) 17.8 / 17.4; 48 rows, two of six of rank 64 (384) 22.1 / 21.8; 820 rows, rank 16, 64 x 3072 (832) 20.5 / 14.3; 8704 rows, rank 64, 64 x 3072 (34816) 342 / 51
-constexpr int64_t kDownPlaces = 512;
 int down_rows(regione_ctx* ctx, const DownCall& d) {
     const int64_t tiles = (d.m + 15) / 16, places = static_cast<int64_t>(d.m < 16 ? d.m : 16) * d.sel * d.blocks;
     if (tiles * places <= kDownPlaces) {
