@@ -342,8 +342,8 @@ int regione_expert_combine(regione_ctx* ctx, const void* rows, int32_t rows_dtyp
  *   elements, made by regione_pack_adapter from A [rank, k] and B [n, rank] (bf16 row-major; smaller adapters padded with
  *   zeros to the common rank); they must be 16-byte aligned.
  *   k a multiple of 64; rank 1..256, n_sel 1..32, n_adapters at most 65536.  bf16 contexts.
- * x A^T is summed in float32, multiplied by its weight and kept as two (y in bf16) or three (y in float32) bf16 terms, to 2^-16
- * and to float32's own precision.  Values that are not finite spoil only the rows that use them: in A all of a row, in B the columns that
+ * x A^T is summed in float32, multiplied by its weight and kept as three bf16 terms that add up to that float32 number,
+ * whatever the type of y.  Values that are not finite spoil only the rows that use them: in A all of a row, in B the columns that
  * hold them, with NaN.  Uses the context's workspace (REGIONE_ERR_WORKSPACE in a context without max_fresh). */
 int64_t regione_packed_adapter_elems(int32_t n, int32_t k, int32_t rank);
 int regione_pack_adapter(regione_ctx* ctx, const void* a, const void* b, int32_t n, int32_t k, int32_t rank, void* packed);

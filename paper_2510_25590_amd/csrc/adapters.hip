@@ -60,15 +60,17 @@ pack_adapter_bad_kernel(const bf16_t* __restrict__ b, int n, int rank, uint32_t*
     }
 }
 
-// w * x[row] A_a^T, w the sum of the row's weights of adapter a, as `terms` bf16 values that add up to it: the value rounded, what is left of it rounded, and so on (2^-8, 2^-16, 2^-24
-// relative at most).  One rounding would be as large as that of a bf16 result, and larger where the projection and the adapter cancel.
-
+// w * x[row] A_a^T, w the sum of the row's weights of adapter a, as kTerms bf16 values: the value rounded, what is left of it rounded, and what is left then.  Of a float32's 24 bits the first leaves at
+// most 16 and the second eight, so that the three add up to it exactly.  One term would be rounded as a bf16 result is, two would leave 2^-17 of the share: where the projection cancels the
+// adapter, all that is left may lie below that.  us, the whole call with a bf16 result, two terms / three: 48 rows with 32 adapters of
+// rank 16, 2048 x 4096, 14.0 / 15.4; 820 rows, two of rank 32 each, 3072 x 12288, 74.3 / 77.0; 8704 rows, rank 64, 3072 x 9216, 395 / 404; 8192 rows with 500 adapters of rank 16, 2048 x 4096, 194 / 236.
+constexpr int kTerms = 3;
 // Four values at ranks 16 * block + 4 * kc on, where at(column) is: the terms' blocks one after the other, filled up to `cols` with zeros.
-template <typename At> __device__ __forceinline__ void put_terms(const At& at, int kc, int block, int blocks, int terms, int cols, float w, const f32x4& sum, bool named = true) {
+template <typename At> __device__ __forceinline__ void put_terms(const At& at, int kc, int block, int blocks, int cols, float w, const f32x4& sum, bool named = true) {
     float left[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) left[e] = named ? w * sum[e] : 0.f;
-    for (int p = 0; p < terms; ++p) {
+    for (int p = 0; p < kTerms; ++p) {
         bf16_t v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -78,11 +80,11 @@ template <typename At> __device__ __forceinline__ void put_terms(const At& at, i
         }
         *reinterpret_cast<uint2*>(at((p * blocks + block) * 16 + 4 * kc)) = make_uint2(v[0] | static_cast<unsigned>(v[1]) << 16, v[2] | static_cast<unsigned>(v[3]) << 16);
     }
-    if (block == blocks - 1 && cols > terms * blocks * 16) *reinterpret_cast<uint2*>(at(terms * blocks * 16 + 4 * kc)) = make_uint2(0u, 0u);
+    if (block == blocks - 1 && cols > kTerms * blocks * 16) *reinterpret_cast<uint2*>(at(kTerms * blocks * 16 + 4 * kc)) = make_uint2(0u, 0u);
 }
 
 constexpr int kDownWaves = 8;
-struct DownCall { const bf16_t* x; const bf16_t* packed; int64_t stride; const int32_t* which; const float* weight; int count, sel, m, k, blocks, terms, cols; bf16_t* t; };
+struct DownCall { const bf16_t* x; const bf16_t* packed; int64_t stride; const int32_t* which; const float* weight; int count, sel, m, k, blocks, cols; bf16_t* t; };
 
 // For the kernel of 16 rows, t [rows, sel, cols], each adapter at the first of the row's places that name it: a workgroup per block of 16 ranks of every place of 16 rows; those whose adapter an earlier place names end at once.  Its eight waves split K and meet in LDS, where the sums are
 // formed in wave order.  One row, K 3072, rank 16 4.0 us, 48 rows with 32 adapters, K 2048 5.5: the launch, the row's adapter, then x and A in one trip to memory.
@@ -134,7 +136,7 @@ adapters_down_rows_kernel(DownCall d) {
 #pragma unroll
     for (int v = 1; v < kDownWaves; ++v) acc += sums[v][lane];
     bf16_t* const row = d.t + (static_cast<int64_t>(m0 + l16) * d.sel + place) * d.cols;
-    put_terms([&](int c) { return row + c; }, kc, block, d.blocks, d.terms, d.cols, w, acc);
+    put_terms([&](int c) { return row + c; }, kc, block, d.blocks, d.cols, w, acc);
 }
 
 // For tiles (their layout and plan: gemm_adapters.h): a workgroup owns 16 * RB rows and goes through the blocks of 16 ranks of their adapters, NB at a time; those of the tile that none of the
@@ -206,7 +208,7 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
     auto place = [&](int row, int of, int c) __attribute__((always_inline)) {       // column c of a block of 16 terms, in the order of LDS
         return t + (static_cast<int64_t>(of >> 2) * tiles.rows + row) * 128 + ((((of & 3) * 2 + (c >> 3)) ^ ((row >> 1) & 7)) << 4) + (c & 7) * 2;
     };
-    const int per = d.terms * d.blocks;                           // blocks of 16 terms of an adapter
+    const int per = kTerms * d.blocks;                            // blocks of 16 terms of an adapter
     int32_t* const plan = tiles.plan + static_cast<int64_t>(tile) * tiles.plan_pitch;
     int64_t* const offsets = reinterpret_cast<int64_t*>(plan + 4);
     const int ids_at = 4 + (tiles.plan_pitch - 4) / 3 * 2;
@@ -333,8 +335,8 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
                             if (ids[row * d.sel + s] == unit_a[q]) { at = s; w += weights[row * d.sel + s]; }
                     if (!PLANNED) {
                         bf16_t* const to = reinterpret_cast<bf16_t*>(t) + (row * d.sel + at) * d.cols;
-                        if (at >= 0) put_terms([&](int c) { return to + c; }, kc, unit_block[q], d.blocks, d.terms, d.cols, w, sum);
-                    } else if (row < place_rows) put_terms([&](int c) { return place(row0 + row, first + (c >> 4), c & 15); }, kc, unit_block[q], d.blocks, d.terms, 0, w, sum, at >= 0);
+                        if (at >= 0) put_terms([&](int c) { return to + c; }, kc, unit_block[q], d.blocks, d.cols, w, sum);
+                    } else if (row < place_rows) put_terms([&](int c) { return place(row0 + row, first + (c >> 4), c & 15); }, kc, unit_block[q], d.blocks, 0, w, sum, at >= 0);
                 }
             __syncthreads();
         }
@@ -438,14 +440,14 @@ extern "C" int regione_linear_adapters(regione_ctx* ctx, const void* x, const vo
     if (!rg_aligned16(x) || !rg_aligned16(w_packed) || !rg_aligned16(adapters_packed)) RG_FAIL(REGIONE_ERR_INVALID_ARG, "linear_adapters: operands must be 16-byte aligned");
 
     const bool y_f32 = out_dtype == REGIONE_FP32;
-    const int blocks = (rank + 15) / 16, terms = y_f32 ? 3 : 2, cols = (terms * blocks * 16 + 31) & ~31;
+    const int blocks = (rank + 15) / 16, cols = (kTerms * blocks * 16 + 31) & ~31;
     const size_t all = ctx->gemm_part_bytes, room = all / 2 < kTermBytes ? (all / 2) & ~size_t{255} : kTermBytes;      // (a context without a workspace has none)
     // the inner products lie at the workspace's end, the sums of K splits in the rest of it
     char* const end = reinterpret_cast<char*>(ctx->gemm_part) + all - room;
     ctx->gemm_part_bytes = all - room;
     AdapterTiles tiles = rg_adapter_tiles(ctx, m, n, k);
     // the most that a tile can name: every row another adapter
-    const int64_t named = static_cast<int64_t>(tiles.rows) * n_sel < n_adapters ? static_cast<int64_t>(tiles.rows) * n_sel : n_adapters, tile_steps = (named * terms * blocks + 3) / 4;
+    const int64_t named = static_cast<int64_t>(tiles.rows) * n_sel < n_adapters ? static_cast<int64_t>(tiles.rows) * n_sel : n_adapters, tile_steps = (named * kTerms * blocks + 3) / 4;
     const int64_t tile_bytes = tile_steps * tiles.rows * 128, plan_words = 4 + 12 * tile_steps, plan_bytes = plan_words * 4, fits = static_cast<int64_t>(room) / (tile_bytes + plan_bytes), m_tiles = (m + tiles.rows - 1) / tiles.rows;
     // More than fits goes through in passes of whole tiles; a tile that does not fit leaves the call to the kernel of 16 rows, which reads what its rows name and no more.  us, passes / that kernel, 500 adapters,
     // 4096 x 2048: 8192 rows, rank 16, a request every 64 rows 180 / 943, every row any adapter 911 / 1095; 2048 rows, rank 64 83 / 340 and 648 / 598 (with 32 MB in place of 64: 260, 1473, 113 and 909)
@@ -472,7 +474,7 @@ extern "C" int regione_linear_adapters(regione_ctx* ctx, const void* x, const vo
     for (int64_t r0 = 0; r0 < m && rc == REGIONE_OK; r0 += chunk) {
         const int rows = static_cast<int>(m - r0 < chunk ? m - r0 : chunk);
         DownCall d = {static_cast<const bf16_t*>(x) + r0 * k, static_cast<const bf16_t*>(adapters_packed), adapter_elems(n, k, blocks), adapter + r0 * n_sel, weight_opt ? weight_opt + r0 * n_sel : nullptr,
-                      n_adapters, n_sel, rows, k, blocks, terms, cols, reinterpret_cast<bf16_t*>(end)};
+                      n_adapters, n_sel, rows, k, blocks, cols, reinterpret_cast<bf16_t*>(end)};
         GemmEpilogue ep = {};
         ep.kind = EPI_PLAIN; ep.bias = b_opt; ep.act = act; ep.act_from = 0;
         ep.y = static_cast<char*>(y) + r0 * n * (y_f32 ? 4 : 2); ep.ldy = n; ep.y_f32 = y_f32;
