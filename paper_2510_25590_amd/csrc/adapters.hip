@@ -70,11 +70,13 @@ template <typename At> __device__ __forceinline__ void put_terms(const At& at, i
     float left[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) left[e] = named ? w * sum[e] : 0.f;
+#pragma unroll
     for (int p = 0; p < kTerms; ++p) {
         bf16_t v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             v[e] = f32_to_bf16(left[e]);
+            if (p == 0) v[e] -= (v[e] & 0x7fff) == 0x7f80 && __builtin_fabsf(left[e]) < INFINITY ? 1 : 0;       // (rounded up past the largest bf16, which is the first term then)
             const float r = bf16_to_f32(v[e]);
             left[e] = __builtin_fabsf(r) < INFINITY ? left[e] - r : 0.f;           // (what is not finite is one term)
         }

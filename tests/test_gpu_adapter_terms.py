@@ -79,3 +79,25 @@ def test_cancelled_bf16_results_of_every_tile(tile, splits):
     for rank, count, k in ((9, 3, 64), (20, 2, 320), (48, 2, 128)):
         Powers(ctx, 270, 260, k, rank, count, 8, tile + rank).check(ctx, torch.bfloat16)
     ctx.close()
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,n", [(3, 64), (45, 2048), (300, 520), (3000, 64)])
+def test_inner_products_above_the_largest_bf16(ctx, m, n, out):
+    """2^128 - 2^118: finite in float32, rounded to bf16 infinite.  B holds 2^-100 in the first column and zeros in the others."""
+    k, rank = 64, 5
+    x, a, b = np.zeros((m, k)), np.zeros((rank, k)), np.zeros((n, rank))
+    x[:, :3] = 1.0
+    a[2, :3] = 2.0 ** 128 - 2.0 ** 120, 2.0 ** 119, 2.0 ** 118
+    b[0, 2] = 2.0 ** -100
+    x[1] *= -1.0
+    total = float(a[2].sum())
+    assert float(np.float32(total)) == total < 2.0 ** 128 and np.isinf(torch.tensor(total, dtype=torch.float32).to(torch.bfloat16).item())
+    bf = lambda v: up(v, torch.bfloat16)
+    ap = rg.pack_adapters(ctx, bf(a[None]), bf(b[None]))
+    wp = rg.pack_weight(ctx, torch.zeros(n, k, dtype=torch.bfloat16, device="cuda"))
+    y = torch.full((m, n), 7.0, dtype=out, device="cuda")
+    rg.regione_linear_adapters(ctx, bf(x), wp, None, ap, torch.zeros(m, 1, dtype=torch.int32, device="cuda"), None, 1, 1, rank, m, n, k, rg.ACT_NONE, rg.FP32 if out == torch.float32 else rg.BF16, y)
+    want = np.zeros((m, n))
+    want[:, 0] = total * 2.0 ** -100 * x[:, 0]
+    assert torch.equal(y.cpu(), torch.from_numpy(want).to(out))
