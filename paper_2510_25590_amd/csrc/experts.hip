@@ -495,7 +495,7 @@ route_kernel(RouteCall c) {
         bool sure = thin > 0.f;
         if (check) {
             const float v = chosen < 0 ? -INFINITY : chosen_logit, b = chosen < 0 ? 0.f : c.bias[chosen];
-            chosen_logit = chosen < 0 ? 0.f : as_float<T>(row[chosen]);
+            chosen_logit = chosen < 0 ? 0.f : __builtin_fminf(as_float<T>(row[chosen]), 3.402823466e38f);      // (as in `logit`: from +infinity every difference is infinite)
             const float next_v = __shfl_down(v, 1, LPT), next_b = __shfl_down(b, 1, LPT), next_x = __shfl_down(chosen_logit, 1, LPT), last_v = __shfl_down(v, 2, LPT);
             const float least = (c.sigmoid ? 0x1p-21f : 0x1p-20f) * (1.f + __builtin_fabsf(v)) + (c.sigmoid ? 0.f : 0x1p-17f * (__builtin_fabsf(v - b) + __builtin_fabsf(next_v - next_b)));
             const bool near = l < c.top_k && next_v > -INFINITY && !(v - next_v > least) && !(next_x == chosen_logit && next_b == b);
