@@ -109,11 +109,13 @@ template <> __device__ __forceinline__ float as_float<bf16_t>(bf16_t v) { return
 struct WideKey {
     typedef double type;
     static constexpr double NONE = -INFINITY;
+    static constexpr int PAST = 0x7fe00000;                                // of 2^1023, past all float32 values, in the place of +infinity, which cannot hold an expert: with other bits set it is NaN
     static __device__ __forceinline__ double make(float v, int expert) {
         v += 0.0f;                                                         // (-0 is as large as 0)
         const double d = static_cast<double>(v);
         const int low = (1023 - expert) ^ ((__float_as_int(v) >> 31) & 1023);
-        return __hiloint2double(__double2hiint(d), v > -INFINITY ? __double2loint(d) | low : 0);
+        const int high = __double2hiint(d) < PAST ? __double2hiint(d) : PAST;
+        return __hiloint2double(high, v > -INFINITY ? __double2loint(d) | low : 0);
     }
     static __device__ __forceinline__ int expert(double k) { return 1023 - ((__double2loint(k) & 1023) ^ ((__double2hiint(k) >> 31) & 1023)); }
     static __device__ __forceinline__ float value(double k) { return static_cast<float>(__hiloint2double(__double2hiint(k), __double2loint(k) & ~1023)); }
