@@ -499,13 +499,17 @@ route_kernel(RouteCall c) {
             const float v = chosen < 0 ? -INFINITY : chosen_logit, b = chosen < 0 ? 0.f : c.bias[chosen];
             chosen_logit = chosen < 0 ? 0.f : __builtin_fminf(as_float<T>(row[chosen]), 3.402823466e38f);      // (as in `logit`: from +infinity every difference is infinite)
             const float next_v = __shfl_down(v, 1, LPT), next_b = __shfl_down(b, 1, LPT), next_x = __shfl_down(chosen_logit, 1, LPT), last_v = __shfl_down(v, 2, LPT);
+            // What two values may be off together, in 2^-24.  Softmax, times the score: 2 each for its exponential and the reciprocal, 1 for their product, 37 for the additions of the sum (32 in a lane, over
+            // 64 of them), 2 + 2.5 ln(1024) for the sum's exponentials, at most 60 in all, and 2.5 |x - top| for the score's exponent, which with the score is at most 0.92.  Sigmoid: 3.5.  For the bias 1
+            // times each value.  `least`: this value and the next; `wide`: this one and any, as two scores add up to 1 at most (`least` there does not know of the other's score).
             const float least = (c.sigmoid ? 0x1p-21f : 0x1p-20f) * (1.f + __builtin_fabsf(v)) + (c.sigmoid ? 0.f : 0x1p-17f * (__builtin_fabsf(v - b) + __builtin_fabsf(next_v - next_b)));
+            const float wide = (c.sigmoid ? 0x1p-21f : 0x1p-18f) * (1.f + __builtin_fabsf(v));
             const bool near = l < c.top_k && next_v > -INFINITY && !(v - next_v > least) && !(next_x == chosen_logit && next_b == b);
             // the last choice and the second one behind it too near: there may be more of them (infinities of one sign: as near as can be)
-            const bool crowded = l == c.top_k - 1 && last_v > -INFINITY && !(v - last_v > least);
+            const bool crowded = l == c.top_k - 1 && last_v > -INFINITY && !(v - last_v > wide);
             if (__ballot(crowded && routed)) {
                 const int from = LPT == 64 ? c.top_k - 1 : (lane & ~(LPT - 1)) + c.top_k - 1;
-                const float edge_v = lane_value<LPT>(v, from), edge_b = lane_value<LPT>(b, from), edge_x = lane_value<LPT>(chosen_logit, from), edge = lane_value<LPT>(least, from);
+                const float edge_v = lane_value<LPT>(v, from), edge_b = lane_value<LPT>(b, from), edge_x = lane_value<LPT>(chosen_logit, from), edge = lane_value<LPT>(wide, from);
                 const bool look = lane_value<LPT>(crowded ? 1 : 0, from) != 0;
 #pragma unroll
                 for (int i = 0; i < EPL; ++i)
