@@ -255,11 +255,14 @@ template <int LPT, int EPL, typename V> __device__ __forceinline__ V group_sum(c
     return c.group_best == 2 && b > static_cast<V>(-INFINITY) ? a + b : a;
 }
 
-// exp(x) to 2^-31, in 64 bits so that nothing but the last rounding counts in float32: 2^n times the exponential's series up to the eighth power of |r| <= ln(2) / 2 (the ninth is 2e-10).
+// exp(x) to 2^-46 (2^-44 for x of hundreds), in 64 bits so that nothing but the last rounding counts in float32: 2^n times the exponential's series up to the eleventh power of |r| <= ln(2) / 2 (the twelfth is 2^-47).
 __device__ __forceinline__ double exp64(double x) {
     x = __builtin_fmin(__builtin_fmax(x, -800.0), 800.0);
     const double n = __builtin_rint(x * 1.4426950408889634), r = __builtin_fma(n, -0.6931471805599453, x);
-    double p = 1.0 / 40320.0;
+    double p = 1.0 / 39916800.0;
+    p = __builtin_fma(p, r, 1.0 / 3628800.0);
+    p = __builtin_fma(p, r, 1.0 / 362880.0);
+    p = __builtin_fma(p, r, 1.0 / 40320.0);
     p = __builtin_fma(p, r, 1.0 / 5040.0);
     p = __builtin_fma(p, r, 1.0 / 720.0);
     p = __builtin_fma(p, r, 1.0 / 120.0);

@@ -1,0 +1,32 @@
+"""Weights are formed in 64 bits and rounded once: half a step of float32 (2^-24), and 2^-44 relative for what comes before."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import expert_reference as ex
+from paper_2510_25590_amd import binding as rg
+from test_gpu_experts import route, up
+
+pytestmark = pytest.mark.gpu
+ONCE = 2.0 ** -24 * (1 + 2.0 ** -20)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return rg.Context(256, 4, 64, 1024, 64, 64)
+
+
+def test_renormalised_weights_next_to_a_power_of_two(ctx):
+    """Weights 1 / (1 + a + b) a little above a half, where half a step is 2^-24 of the value and an exponential that is off by 2^-32 shows; a is exp of about -ln(2) / 2, the hardest for a series around
+    multiples of ln(2)."""
+    rng = np.random.default_rng(0)
+    n = 1 << 18
+    a = (-0.3465 + 0.001 * rng.random(n)).astype(np.float32)
+    total = 2.0 / (1.0 + 0.001 * rng.random(n))
+    b = np.log(total - 1.0 - np.exp(a.astype(np.float64))).astype(np.float32)
+    l = np.stack([a, np.zeros(n, np.float32), b], axis=1)
+    expert, weight = route(ctx, up(l), None, None, "softmax", 1, 1, 1, 3, True, 1.0)
+    assert (expert == [1, 0, 2]).all()
+    p = np.exp(l[:, [1, 0, 2]].astype(np.float64))
+    want = p / p.sum(axis=1, keepdims=True)
+    assert np.max(np.abs(weight - want) / want) <= ONCE
