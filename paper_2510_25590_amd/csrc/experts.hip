@@ -474,10 +474,11 @@ route_kernel(RouteCall c) {
         }
     } else {
         if (!c.sigmoid && !c.renormalise) {
-            float sum = 0.f;
+            // (in 64 bits, as with bias or groups: in float32 a weight of 128 experts is off by up to three half steps.  65536 tokens, bf16, float32 / this
+            // 14.9 / 19.1 us)
 #pragma unroll
-            for (int i = 0; i < EPL; ++i) sum += logit[i] == -INFINITY ? 0.f : expf(__builtin_fminf(logit[i], 3.402823466e38f) - top);
-            all = lanes_sum<LPT>(sum);
+            for (int i = 0; i < EPL; ++i) all += logit[i] == -INFINITY ? 0.0 : exp64(static_cast<double>(__builtin_fminf(logit[i], 3.402823466e38f)) - static_cast<double>(top));
+            all = lanes_sum<LPT>(all);
         }
 #pragma unroll
         for (int i = 0; i < EPL; ++i) key[i] = make_key(logit[i], expert0 + i);

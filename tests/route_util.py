@@ -5,8 +5,8 @@ import torch
 from oracle import expert_reference as ex
 from test_gpu_experts import route, up
 
-# Weights are formed in 64 bits and rounded once: half a step of float32, and 2^-31 for two exponentials of 2^-32 each
-WEIGHT = 2.0 ** -24 * (1 + 2.0 ** -7)
+# Weights are formed in 64 bits and rounded once: half a step of float32, and 2^-44 for what comes before
+WEIGHT = 2.0 ** -24 * (1 + 2.0 ** -20)
 
 
 def check_repeated(ctx, rows, tokens, bias, score, groups, top_groups, best, k, renorm, scale, mask=None, weight=WEIGHT):

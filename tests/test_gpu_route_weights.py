@@ -30,3 +30,19 @@ def test_renormalised_weights_next_to_a_power_of_two(ctx):
     p = np.exp(l[:, [1, 0, 2]].astype(np.float64))
     want = p / p.sum(axis=1, keepdims=True)
     assert np.max(np.abs(weight - want) / want) <= ONCE
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens", [300, 2047, 2048, 4099])
+@pytest.mark.parametrize("experts", [7, 64, 128, 200, 256, 1000])
+def test_softmax_over_all_experts(ctx, experts, tokens, dtype):
+    """... not renormalised, without bias and groups: the sum over all experts in 64 bits too."""
+    rng = np.random.default_rng(experts + tokens)
+    logits = up(1.5 * rng.normal(size=(tokens, experts)), torch.float32).to(dtype)
+    k = min(experts, 8)
+    expert, weight = route(ctx, logits, None, None, "softmax", 1, 1, 1, k, False, 2.5)
+    l = logits.cpu().double().numpy()
+    assert np.array_equal(expert, np.argsort(-l, axis=1, kind="stable")[:, :k])
+    p = np.exp(l - l.max(axis=1, keepdims=True))
+    want = 2.5 * np.take_along_axis(p / p.sum(axis=1, keepdims=True), expert.astype(np.int64), axis=1)
+    assert np.max(np.abs(weight - want) / want) <= ONCE
