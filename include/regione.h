@@ -318,7 +318,8 @@ int regione_linear_mxfp4_grouped(regione_ctx* ctx, const void* xq, const void* x
  * regione_expert_slots: a stable sort of the pairs (token, j) by expert[token, j]; entries outside [0, n_experts) belong to none.
  *   group_offsets [n_experts + 1] int32: first row of every expert, and the end;  row_token [n_tokens * top_k] int32: the token
  *   of each row, ascending within an expert (entries past the end stay as they were);  slot [n_tokens, top_k] int32: the
- *   row of each pair, -1 for none.
+ *   row of each pair, -1 for none.  More than 4096 pairs use the context's workspace (REGIONE_ERR_WORKSPACE in a context without
+ *   max_fresh); nothing else here does.
  * regione_expert_combine: out[t] = base[t] + sum over j of weight[t, j] * rows[slot[t, j]], in float32 in the order of j, rounded
  *   once; slots outside [0, n_rows) add nothing.  rows [n_rows, cols] of rows_dtype; weight_opt NULL: 1; base_opt
  *   [n_tokens, cols] of out_dtype, may be `out` itself, NULL: 0; out [n_tokens, cols] of out_dtype.  rows and out must not overlap. */
