@@ -311,7 +311,8 @@ int regione_linear_mxfp4_grouped(regione_ctx* ctx, const void* xq, const void* x
  *   expert [n_tokens, top_k] int32: the experts of the largest c in falling order, of equal ones the lowest first, for groups as
  *   well; without a bias experts are compared by their logits, which the scores grow with.  An expert whose logit or value is NaN
  *   or -infinity is never chosen; a logit of +infinity counts as the largest float32.
- *   weight [n_tokens, top_k] float32: scale * s, with `renormalise` scale * s / (sum of the token's chosen s; 0 if that is 0).
+ *   weight [n_tokens, top_k] float32: scale * s, with `renormalise` scale * s / (sum of the token's chosen s; 0 if that is 0: the
+ *   sigmoid of a logit counts as 0 from -709 down, the softmax never does here).
  *   Where fewer than top_k experts can be chosen the last entries are expert -1, weight 0; so are all entries of a token
  *   whose mask_opt [n_tokens] uint8 is 0.
  *   n_groups divides n_experts (at most 64 groups), top_k <= top_groups * n_experts / n_groups.

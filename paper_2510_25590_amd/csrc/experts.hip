@@ -273,10 +273,10 @@ __device__ __forceinline__ double exp64(double x) {
     p = __builtin_fma(p, r, 1.0);
     return __builtin_ldexp(p, static_cast<int>(n));
 }
-// 1 / x for x of ordinary size, to about 2^-45: the reciprocal instruction and one step of Newton's
+// 1 / x for x of 2^-1023 to 2^1023, to about 2^-45: the reciprocal instruction and one step of Newton's; 0 for infinity
 __device__ __forceinline__ double over64(double x) {
     const double r = __builtin_amdgcn_rcp(x);
-    return x > 0x1p1000 ? 0.0 : __builtin_fma(r, __builtin_fma(-x, r, 1.0), r);
+    return x < INFINITY ? __builtin_fma(r, __builtin_fma(-x, r, 1.0), r) : 0.0;
 }
 
 // The choice in 64 bits.  Returns the expert and sets its logit in lane j.
@@ -539,7 +539,7 @@ route_kernel(RouteCall c) {
     const bool has = routed && chosen >= 0;
     double w = 0.0;
     if (c.sigmoid) {
-        w = has ? over64(1.0 + exp64(-static_cast<double>(chosen_logit))) : 0.0;
+        w = has && chosen_logit > -709.f ? over64(1.0 + exp64(-static_cast<double>(chosen_logit))) : 0.0;       // (e^709 is 2^1022.9)
     } else {
         const float from = c.renormalise ? lanes_max<LPT>(has ? chosen_logit : -INFINITY) : top;
         w = has ? exp64(static_cast<double>(chosen_logit) - static_cast<double>(from)) : 0.0;

@@ -3,8 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import expert_reference as ex
 from paper_2510_25590_amd import binding as rg
+from route_util import check_repeated
 from test_gpu_experts import route, up
 
 pytestmark = pytest.mark.gpu
@@ -46,3 +46,17 @@ def test_softmax_over_all_experts(ctx, experts, tokens, dtype):
     p = np.exp(l - l.max(axis=1, keepdims=True))
     want = 2.5 * np.take_along_axis(p / p.sum(axis=1, keepdims=True), expert.astype(np.int64), axis=1)
     assert np.max(np.abs(weight - want) / want) <= ONCE
+
+
+@pytest.mark.parametrize("tokens", [7, 2047, 2048, 4099])
+@pytest.mark.parametrize("k", [1, 3, 8])
+def test_renormalised_sigmoids_far_below_one(ctx, k, tokens):
+    """Scores of 1e-300 and less, whose reciprocals pass 2^1000; they count as 0 from e^-709 on.  Two exponentials of arguments of hundreds are off by 2^-44 together, and a quarter more for what is behind them."""
+    l = np.full((7, 8), -720.0, np.float32)
+    l[0] = -690.0 - 0.1 * np.arange(8)
+    l[1] = -693.0 - 0.25 * np.arange(8)
+    l[2] = -700.0 + 0.3 * np.arange(8)
+    l[3] = -708.96875 + 0.03125 * np.arange(8)
+    l[4, :3] = -709.0, -708.5, -709.03125
+    l[5, 5] = -650.0
+    check_repeated(ctx, up(l), tokens, None, "sigmoid", 1, 1, 1, k, True, 1.0, weight=2.0 ** -24 * (1 + 2.0 ** -19))
