@@ -1,5 +1,5 @@
-// Low-rank adapters of many requests beside a shared projection: packing, and the inner products of every row with its adapters' A.  What they bring to the result is added at the end
-// of the projection's tiles (gemm_adapters.h).
+// Low-rank adapters of many requests beside a shared projection: packing, and the inner products of every row with its adapters' A.  What they bring to the result are further
+// K-steps of the projection's tiles (gemm_adapters.h).
 #include "gemm_adapters.h"
 
 namespace {

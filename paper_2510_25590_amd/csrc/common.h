@@ -104,7 +104,7 @@ __device__ __forceinline__ bf16_t f32_to_bf16(float f) {
 }
 
 // ---- internal launchers (each enqueues on ctx->stream and returns an error code)
-enum { EPI_PLAIN = 0, EPI_QKV = 1, EPI_RESID = 2, EPI_VELOCITY = 3, EPI_ADAPTERS = 4 };      // EPI_ADAPTERS: EPI_PLAIN behind the adapters' share (gemm_adapters.h)
+enum { EPI_PLAIN = 0, EPI_QKV = 1, EPI_RESID = 2, EPI_VELOCITY = 3, EPI_ADAPTERS = 4 };      // EPI_ADAPTERS: EPI_PLAIN, the adapters' K-steps behind the product's (gemm_adapters.h)
 
 // Low-rank adapters of a product's rows (gemm_adapters.h): which [rows, sel] their adapters (none: outside [0, count)), b the packed B of adapter 0 and bad the bits of its columns that hold
 // values that are not finite, those of the others `stride` elements further each; blocks: of 16 ranks; cols: the terms' blocks, filled up to 32 with zeros.  t: the inner products with A in

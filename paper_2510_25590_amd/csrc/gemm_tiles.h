@@ -8,7 +8,7 @@ int rg_gemm_tile_wide(regione_ctx* ctx, int tile, const bf16_t* a, int lda, cons
 int rg_gemm_tile_128(regione_ctx* ctx, int tile, const bf16_t* a, int lda, const bf16_t* wp, int m, int n, int k, int splits, const GemmEpilogue& ep);
 int rg_gemm_tile_96(regione_ctx* ctx, int tile, const bf16_t* a, int lda, const bf16_t* wp, int m, int n, int k, int splits, const GemmEpilogue& ep);
 int rg_gemm_tile_kg(regione_ctx* ctx, int tile, const bf16_t* a, int lda, const bf16_t* wp, int m, int n, int k, int splits, const GemmEpilogue& ep);
-// behind the product the rows' low-rank adapters (bf16, EPI_ADAPTERS)
+// the steps of the rows' low-rank adapters behind the product's (bf16, EPI_ADAPTERS)
 int rg_gemm_tile_adapters(regione_ctx* ctx, int tile, const bf16_t* a, int lda, const bf16_t* wp, int m, int n, int k, int splits, const GemmEpilogue& ep);
 int rg_gemm_tile_adapters_narrow(regione_ctx* ctx, int tile, const bf16_t* a, int lda, const bf16_t* wp, int m, int n, int k, int splits, const GemmEpilogue& ep);
 // E4M3 operands; lda and k count pairs of values

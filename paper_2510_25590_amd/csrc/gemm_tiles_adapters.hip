@@ -1,4 +1,4 @@
-// The wide tiles of the two-group GEMM with low-rank adapters at their end (gemm_adapters.h).
+// The wide tiles of the two-group GEMM with low-rank adapters' K-steps behind the product's (gemm_adapters.h).
 #include "gemm_launch.h"
 
 #define RG_TILE_ADAPTERS(CODE, LAUNCH, ...) if (tile == CODE) return LAUNCH<__VA_ARGS__, EPI_ADAPTERS>(ctx, a, lda, wp, m, n, k, splits, ep);

@@ -1,4 +1,4 @@
-// The 64-, 96- and 128-column tiles of the two-group GEMM with low-rank adapters at their end (gemm_adapters.h).
+// The 64-, 96- and 128-column tiles of the two-group GEMM with low-rank adapters' K-steps behind the product's (gemm_adapters.h).
 #include "gemm_launch.h"
 
 #define RG_TILE_ADAPTERS(CODE, ...) if (tile == CODE) return launch_kg<__VA_ARGS__, EPI_ADAPTERS>(ctx, a, lda, wp, m, n, k, splits, ep);
