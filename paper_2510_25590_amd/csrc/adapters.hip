@@ -89,7 +89,7 @@ constexpr int kDownWaves = 8;
 struct DownCall { const bf16_t* x; const bf16_t* packed; int64_t stride; const int32_t* which; const float* weight; int count, sel, m, k, blocks, cols; bf16_t* t; };
 
 // For the kernel of 16 rows, t [rows, sel, cols], each adapter at the first of the row's places that name it: a workgroup per block of 16 ranks of every place of 16 rows; those whose adapter an earlier place names end at once.  Its eight waves split K and meet in LDS, where the sums are
-// formed in wave order.  One row, K 3072, rank 16 4.0 us, 48 rows with 32 adapters, K 2048 5.5: the launch, the row's adapter, then x and A in one trip to memory.
+// formed in wave order.  One row, K 3072, rank 16 4.0 us, 48 rows with 32 adapters, K 2048 5.2: the launch, the row's adapter, then x and A in one trip to memory.
 __global__ void __launch_bounds__(kDownWaves * 64)
 adapters_down_rows_kernel(DownCall d) {
     constexpr int AHEAD = 8;
@@ -144,7 +144,7 @@ adapters_down_rows_kernel(DownCall d) {
 // For tiles (their layout and plan: gemm_adapters.h): a workgroup owns 16 * RB rows and goes through the blocks of 16 ranks of their adapters, NB at a time; those of the tile that none of the
 // rows names are zeros there.  Without a plan (many rows for the kernel of 16): the layout above, every workgroup's rows by themselves.  Workgroups of the same rows (blockIdx.y) take turns.  WAVES waves split K and meet in LDS, where the sums are formed in wave order.
 // The rows come in whole lines, 8 x 128 bytes to a load, and change to fragments in a part of LDS that is the wave's own.  What bounds it is the way from L2 into a CU, 20 bytes a cycle: all of A
-// for every workgroup beside its rows, so that 32 rows to a workgroup pay where there are workgroups enough.  8704 rows, K 3072, rank 64: 24 us (33 with x from HBM), 6 of them the launch and the list of the
+// for every workgroup beside its rows, so that 32 rows to a workgroup pay where there are workgroups enough.  8704 rows, K 3072, rank 64: 22 us (33 with x from HBM), 6 of them the launch and the list of the
 // adapters; with A from L1 20, with x from L1 too 18.  As fragments from memory, 64 bytes of 16 rows to a load, x took half as long again.
 // Steps past a wave's own are multiplied with zeros: a branch around the products lets the compiler move the loads into it, behind all that should hide them.
 struct DownTiles { int rows, plan_pitch; int64_t tile_elems; int32_t* plan; int64_t bad; };      // rows of a tile; elements of an adapter ahead of its bits
@@ -357,8 +357,8 @@ adapters_down_tiles_kernel(DownCall d, DownTiles tiles) {
 }
 
 // Places with their blocks of ranks, of all the 16 rows, up to which each has a workgroup: it fills the chip where rows name many adapters, and loads what the earlier places of its 16 rows load as well.  us, the
-// whole call, a workgroup to a place (adapters_down_rows_kernel) / the other kernel: 40 rows, two of 64 adapters of rank 16 each, 3072 x 3072 (96 places) 20.5 / 29.3; 128 rows, two of eight, 2048 x 2048 (256) 15.7 / 17.9; 64 rows, one of
-// four of rank 64, 3072 x 3072 (256) 17.8 / 17.4; 48 rows, two of six of rank 64 (384) 22.1 / 21.8; 820 rows, rank 16, 64 x 3072 (832) 20.5 / 14.3; 8704 rows, rank 64, 64 x 3072 (34816) 342 / 51
+// whole call, a workgroup to a place (adapters_down_rows_kernel) / the other kernel: 40 rows, two of 64 adapters of rank 16 each, 3072 x 3072 (96 places) 21.9 / 29.0; 128 rows, two of eight, 2048 x 2048 (256) 14.3 / 15.9; 64 rows, one of
+// four of rank 64, 3072 x 3072 (256) 16.6 / 16.2; 48 rows, two of six of rank 64 (384) 24.1 / 25.7; 820 rows, rank 16, 64 x 3072 (832) 18.7 / 12.6; 8704 rows, rank 64, 64 x 3072 (34816) 346 / 51
 constexpr int64_t kDownPlaces = 512;
 template <bool PLANNED, int RB, int NB, int WAVES>
 void launch_down(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
@@ -368,9 +368,9 @@ void launch_down(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
     hipLaunchKernelGGL((adapters_down_tiles_kernel<PLANNED, RB, NB, WAVES>), dim3(pieces, static_cast<unsigned>(batches < room ? batches : room)), dim3(WAVES * 64), 0, ctx->stream, d, tiles);
 }
 template <bool PLANNED> void launch_down(regione_ctx* ctx, const DownCall& d, const DownTiles& tiles) {
-    // us, K 3072, a block of ranks to a workgroup / four / four of 32 rows: 820 rows, rank 16 6.5 / 8.2 / 10.1, rank 64 10.9 / 10.3 / 12.3; 2048 rows, rank 16 6.8 / 8.2 / 9.8, rank 64
-    // 12.6 / 10.5 / 12.1; 4096 rows, rank 16 10.8 / 9.1 / 10.4, rank 64 18.1 / 12.1 / 12.7; 6144 rows, rank 64 24.9 / 16.8 / 14.8; 8704 rows, rank 64 46 / 24.7 / 24.4; 16384 rows 68 / 43 / 34
-    // A block of ranks to a workgroup only where all that 16 rows may name have one: 1711 rows, any of 23 adapters of rank 9, K 320, four workgroups to 16 rows, 20.7 us against 16.1
+    // us, K 3072, a block of ranks to a workgroup / four / four of 32 rows: 820 rows, rank 16 7.0 / 8.8 / 11.1, rank 64 9.1 / 10.5 / 12.5; 2048 rows, rank 16 7.2 / 8.6 / 10.2, rank 64
+    // 10.0 / 10.5 / 12.2; 4096 rows, rank 16 9.2 / 9.9 / 11.4, rank 64 19.0 / 11.9 / 14.0; 6144 rows, rank 64 29.4 / 17.3 / 14.8; 8704 rows, rank 64 45 / 23.6 / 21.6; 16384 rows 61 / 31 / 24
+    // A block of ranks to a workgroup only where all that 16 rows may name have one: 1711 rows, any of 23 adapters of rank 9, K 320, four workgroups to 16 rows, 19.8 us against 13.1
     const int64_t pieces = (d.m + 15) / 16, most = static_cast<int64_t>(16) * d.sel < d.count ? static_cast<int64_t>(16) * d.sel : d.count;
     if (pieces * most * d.blocks <= kDownPlaces) launch_down<PLANNED, 1, 1, 8>(ctx, d, tiles);
     else if (pieces <= 256) launch_down<PLANNED, 1, 4, 4>(ctx, d, tiles);
@@ -452,7 +452,7 @@ extern "C" int regione_linear_adapters(regione_ctx* ctx, const void* x, const vo
     const int64_t named = static_cast<int64_t>(tiles.rows) * n_sel < n_adapters ? static_cast<int64_t>(tiles.rows) * n_sel : n_adapters, tile_steps = (named * kTerms * blocks + 3) / 4;
     const int64_t tile_bytes = tile_steps * tiles.rows * 128, plan_words = 4 + 12 * tile_steps, plan_bytes = plan_words * 4, fits = static_cast<int64_t>(room) / (tile_bytes + plan_bytes), m_tiles = (m + tiles.rows - 1) / tiles.rows;
     // More than fits goes through in passes of whole tiles; a tile that does not fit leaves the call to the kernel of 16 rows, which reads what its rows name and no more.  us, passes / that kernel, 500 adapters,
-    // 4096 x 2048: 8192 rows, rank 16, a request every 64 rows 180 / 943, every row any adapter 911 / 1095; 2048 rows, rank 64 83 / 340 and 648 / 598 (with 32 MB in place of 64: 260, 1473, 113 and 909)
+    // 4096 x 2048: 8192 rows, rank 16, a request every 64 rows 206 / 772, every row any adapter 1290 / 1210; 2048 rows, rank 64 78 / 266 and 746 / 599
     int64_t chunk = m;
     if (tiles.tile && fits < m_tiles) {
         if (fits > 0) {

@@ -9,9 +9,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMostExperts = 1024, kMostChosen = 32, kMostGroups = 64;
 constexpr int64_t kMostPairs = int64_t{1} << 24;             // rows that a grouped product takes
-// Tokens from which on four share a wave, without and with scores to look at beside the logits (bias, groups).  us, a wave to a token / to four: 64 experts, float32, 6 chosen, 1024 tokens 3.7 / 3.6, 4608
-// 4.9 / 4.0, 65536 27.5 / 11.3; 256 experts, bf16, 8 chosen, 1024 tokens 4.7 / 5.0, 2048 5.2 / 5.1, 65536 46 / 21; 256 experts in 8 groups with a bias, 8 chosen, 1024 tokens 7.0 / 9.0, 4608 10.9 / 11.4,
-// 8192 14.5 / 12.5, 65536 79 / 50
+// Tokens from which on four share a wave, without and with scores to look at beside the logits (bias, groups).  us, a wave to a token / to four: 64 experts, float32, 6 chosen, 1024 tokens 3.6 / 3.4, 4608
+// 4.8 / 3.8, 65536 29.6 / 11.0; 256 experts, bf16, 8 chosen, 1024 tokens 4.7 / 4.8, 2048 5.1 / 4.8, 65536 49 / 21; 256 experts in 8 groups with a bias, 8 chosen, 1024 tokens 6.9 / 8.8, 4608 10.4 / 10.7,
+// 8192 13.9 / 12.1, 65536 85 / 52
 constexpr int64_t kRouteShared = 2048, kRouteSharedScored = 8192;
 
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
@@ -369,8 +369,8 @@ __device__ __forceinline__ void put_in_order(const RouteCall& c, const float (&l
 // Without bias and groups the scores lie in the order of the logits (SCORED false).  With them the choice is that of values in 64 bits: in 32 bits the rounding of the exponential would decide
 // between experts that differ by less, and another order of the same operations would choose others.  It is made in 32 bits all the same, and made again in 64 where that cannot be sure: where
 // two values that follow each other in the choice, or the last group that stays and the first that does not, are closer than the errors of both.  (Equal values of equal logits and biases are.)
-// What bounds it: instructions, and for few tokens the chain of maxima.  Kernel trace, us: one token of 64 experts 2.3; 65536 tokens of 128 experts, bf16, 8 chosen, 12.4 (1.7 TB/s; 380 vector instructions per
-// wave of four tokens); 4608 tokens of 256 experts, float32, in 8 groups with a bias, 10 to 11.6 (770 per wave and token).
+// What bounds it: instructions, and for few tokens the chain of maxima.  Kernel trace, us: one token of 64 experts 2.3; 65536 tokens of 128 experts, bf16, 8 chosen, 11.3 to 12.7 (1.7 TB/s; 390 vector instructions per
+// wave of four tokens); 4608 tokens of 256 experts, float32, in 8 groups with a bias, 10 to 11 (790 per wave and token).
 template <typename T, int LPT, int EPL, bool SCORED>
 __global__ void __launch_bounds__(kThreads)
 route_kernel(RouteCall c) {
@@ -725,6 +725,7 @@ place_pairs_kernel(const int32_t* __restrict__ expert, int64_t n, int64_t per_ch
 
 // out[t] = base[t] + sum over j of weight[t, j] * rows[slot[t, j]], in the order of j, float32 in registers, one rounding.  A wave owns 64 * N columns of a token: whole lines of every row, each read
 // once, past the caches.  HBM bounds it: 16384 tokens of four rows of 4096 columns and a base, bf16, 805 MB, 136 us, 5.9 TB/s.
+// Where widths or addresses are no whole pieces of 16 bytes, a column to a lane: loads of two or four bytes bound it then.  The same with 4095 columns 481 us (1.7 TB/s), in float32 344 against 274.
 template <typename T> struct Loaded;
 template <> struct Loaded<bf16_t> { typedef u32x4 type; static constexpr int N = 8; };
 template <> struct Loaded<float> { typedef f32x4 type; static constexpr int N = 4; };

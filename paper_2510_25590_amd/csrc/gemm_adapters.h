@@ -6,7 +6,7 @@
 //
 // Tiles (gemm_pp.h) take the terms as K-steps behind the product's own: for every adapter that a row of the tile names, in ascending order, its terms in all of the tile's rows, zeros in those
 // that do not name it, in the order that a step has in LDS, the tile's steps one after the other.  As steps of the same loop they cost what K costs, and their first loads fly under the
-// product's last steps: 4096 x 2048 x 2048, six steps of eight adapters behind 32, 35.6 -> 42.0 us; 820 x 12288 x 3072, up to six behind 48, 57.9 -> 65.3.  Summed at the end of the tile, each
+// product's last steps: 4096 x 2048 x 2048, six steps of eight adapters behind 32, 35.7 -> 41.6 us; 820 x 12288 x 3072, up to nine behind 48, 59.1 -> 68.3.  Summed at the end of the tile, each
 // wave its rows and their adapters, they waited for memory step by step, 1.7 us each.
 // The plan of a tile, 32-bit words: the number of its steps, whether one of its adapters has values in B that are not finite, where its adapters stand, one unused; then for each 16 terms where
 // the block of 16 ranks of B that they meet begins (64 bits), and for each 16 terms the adapter.

@@ -337,7 +337,7 @@ gemm_pp_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
         a_rd = a_rd == 2 * T::A_STEP ? 0 : a_rd + T::A_STEP;                                                \
     }
     // (the copies run two steps ahead: up to there they are the product's own)
-    // with adapters always all of a wave's rows (those past M bring anything and are not stored): a second form of each loop costs registers that they need; us, the whole call: 8704 x 9216 x 3072
+    // with adapters always all of a wave's rows (those past M bring anything and are not stored): a second form of each loop costs registers that they need; us, the whole call, of an adapter's rank two terms: 8704 x 9216 x 3072
     // rank 64 414 -> 407, rank 16 390 -> 385, 4096 x 2048 x 2048 55.7 -> 54.4
     const int n_plain = KIND == EPI_ADAPTERS ? (n_own < 2 ? 0 : n_own - 2) : n_steps;
     if (KIND == EPI_ADAPTERS || live == RF) { PP_LOOP(0, n_plain, RF, PP_COPY_A, PP_COPY_W) } else { PP_LOOP(0, n_plain, live, PP_COPY_A, PP_COPY_W) }
@@ -559,7 +559,7 @@ gemm_kg_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__
         pp_barrier();                                                                                       \
     }
     // (the copies run NS - 1 steps ahead: up to there they are the product's own)
-    // with adapters always all of a wave's rows: a second form of each loop costs scalar registers that they need, and 820 x 12288 x 3072 83 -> 73 us without
+    // with adapters always all of a wave's rows: a second form of each loop costs scalar registers that they need; 820 x 12288 x 3072, of an adapter's rank two terms, 83 -> 73 us without
     const int n_plain = KIND == EPI_ADAPTERS ? (n_own < NS - 1 ? 0 : n_own - (NS - 1)) : n_steps;
     if (KIND == EPI_ADAPTERS || live == RF) { KG_LOOP(0, n_plain, RF, KG_COPY) } else { KG_LOOP(0, n_plain, live, KG_COPY) }
     if constexpr (KIND == EPI_ADAPTERS) {
